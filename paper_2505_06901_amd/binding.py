@@ -24,6 +24,8 @@ EXPORTS = [
     "ecco_pb_fit", "ecco_pb_model_create", "ecco_pb_model_S", "ecco_pb_model_texp", "ecco_pb_model_centroids",
     "ecco_pb_model_code_lens", "ecco_pb_model_kp_lens", "ecco_pb_model_to_device", "ecco_pb_model_free",
     "ecco_pb_encode", "ecco_pb_decode", "ecco_pb_decode_gemv", "ecco_pb_model_save", "ecco_pb_model_load",
+    "ecco_kv_pages_take", "ecco_kv_pages_release", "ecco_kv_append_paged", "ecco_kv_append_paged_minmax", "ecco_kv_attend_paged",
+    "ecco_kv_attend_paged_workspace",
 ]
 
 
@@ -86,6 +88,14 @@ def lib():
         L.ecco_pb_decode.argtypes = [vp, vp, sz, vp, vp]
         L.ecco_pb_decode_gemv.argtypes = [vp, vp, i32, i32, vp, vp, vp]
         L.ecco_act_decode.argtypes = [vp, sz, vp, vp]
+        i64 = C.c_int64
+        L.ecco_kv_pages_take.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
+        L.ecco_kv_pages_release.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, vp, i32, vp]
+        for name in ("ecco_kv_append_paged", "ecco_kv_append_paged_minmax"):
+            getattr(L, name).argtypes = [vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp]
+        L.ecco_kv_attend_paged_workspace.argtypes = [i32] * 7 + [i64]
+        L.ecco_kv_attend_paged_workspace.restype = sz
+        L.ecco_kv_attend_paged.argtypes = [vp, vp, vp, i64] + [vp] * 7 + [i32] * 9 + [i64, vp, sz, vp, i32, vp]
         _lib = L
     return _lib
 
@@ -332,6 +342,110 @@ def ecco_act_decode(blocks, dst=None):
         dst = torch.empty((n, ACT_GROUP), dtype=torch.float16, device=blocks.device)
     _check(lib().ecco_act_decode(_dp(blocks), n, _dp(dst), _stream()), "ecco_act_decode")
     return dst
+
+
+# ---- the compressed cache in pages (include/ecco_paged.h) ---------------------------------------------------------
+def _int32(*tensors):
+    import torch
+    for t in tensors:
+        assert t is None or t.dtype == torch.int32, "int32 tensors expected"
+
+
+def _rows(x):
+    """(pointer, values from row to row) of a CUDA FP16 tensor [rows, heads, 128] whose rows are contiguous."""
+    import torch
+    assert x.is_cuda and x.dtype == torch.float16 and x.dim() == 3 and x.shape[2] == GROUP
+    assert x.numel() == 0 or x[0].is_contiguous(), "a row's heads must be contiguous"
+    return x.data_ptr(), (x.stride(0) if x.shape[0] > 1 else x.shape[1] * GROUP)
+
+
+def _pool(k_blocks, k_meta, v_blocks, v_meta):
+    """(pages, heads, tokens of a page) of a pool's tensors."""
+    import torch
+    assert k_meta.dim() == 3 and v_meta.shape == k_meta.shape, "meta words are [n_pages, heads, page_tokens]"
+    for blocks in (k_blocks, v_blocks):
+        assert blocks.dtype == torch.uint8 and blocks.numel() == k_meta.numel() * BLOCK_BYTES, "64 bytes per meta word"
+    assert k_meta.element_size() == 4 and v_meta.element_size() == 4
+    return k_meta.shape
+
+
+def ecco_kv_pages_take(seq_len, new_len, page_table, free_pages, free_count, page_tokens: int, n_tokens: int, free_left=None, q_start=None,
+                       kv_len=None, slots=None):
+    """seq_len, new_len int32 [B]; page_table int32 [B, max_pages], updated in place; free_pages int32 [n_pages]; free_count int32 [1], updated
+    in place unless free_left is another tensor.  Returns (q_start [B + 1], kv_len [B], slots [n_tokens])."""
+    import torch
+    B, max_pages = page_table.shape
+    assert seq_len.numel() == B and new_len.numel() == B
+    q_start = torch.empty((B + 1,), dtype=torch.int32, device=page_table.device) if q_start is None else q_start
+    kv_len = torch.empty((B,), dtype=torch.int32, device=page_table.device) if kv_len is None else kv_len
+    slots = torch.empty((n_tokens,), dtype=torch.int32, device=page_table.device) if slots is None else slots
+    free_left = free_count if free_left is None else free_left
+    _int32(seq_len, new_len, page_table, free_pages, free_count, free_left, q_start, kv_len, slots)
+    assert q_start.numel() >= B + 1 and kv_len.numel() >= B and slots.numel() >= n_tokens
+    _check(lib().ecco_kv_pages_take(_dp(seq_len), _dp(new_len), B, page_tokens, max_pages, _dp(page_table), _dp(free_pages), _dp(free_count),
+                                    _dp(free_left), free_pages.numel(), n_tokens, _dp(q_start), _dp(kv_len), _dp(slots), _stream()), "ecco_kv_pages_take")
+    return q_start, kv_len, slots
+
+
+def ecco_kv_pages_release(seq_len, keep_len, page_table, free_pages, free_count, page_tokens: int, free_left=None):
+    """Pages of the tokens keep_len .. seq_len go back onto free_pages; free_count is updated in place unless free_left is another tensor."""
+    B, max_pages = page_table.shape
+    assert seq_len.numel() == B and keep_len.numel() == B
+    free_left = free_count if free_left is None else free_left
+    _int32(seq_len, keep_len, page_table, free_pages, free_count, free_left)
+    _check(lib().ecco_kv_pages_release(_dp(seq_len), _dp(keep_len), B, page_tokens, max_pages, _dp(page_table), _dp(free_pages), _dp(free_count),
+                                       _dp(free_left), free_pages.numel(), _stream()), "ecco_kv_pages_release")
+    return free_left
+
+
+def _append_paged(name: str, mk: Model, mv: Model, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots):
+    n_pages, H, page_tokens = _pool(k_blocks, k_meta, v_blocks, v_meta)
+    assert k_new.shape == v_new.shape and k_new.shape[1] == H and slots.numel() >= k_new.shape[0]
+    _int32(slots)
+    (k, k_stride), (v, v_stride) = _rows(k_new), _rows(v_new)
+    _check(getattr(lib(), name)(mk.handle, mv.handle, k, v, k_stride, v_stride, _dp(k_blocks), _dp(k_meta), _dp(v_blocks), _dp(v_meta), _dp(slots),
+                                k_new.shape[0], H, n_pages, page_tokens, _stream()), name)
+
+
+def ecco_kv_append_paged(mk: Model, mv: Model, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots):
+    """k_new, v_new: CUDA FP16 [n_tokens, H, 128], views into a wider tensor allowed; pools [n_pages, H, page_tokens]; slots int32 [n_tokens]."""
+    _append_paged("ecco_kv_append_paged", mk, mv, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots)
+
+
+def ecco_kv_append_paged_minmax(mk: Model, mv: Model, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots):
+    """As ecco_kv_append_paged, with the min/max pattern selector."""
+    _append_paged("ecco_kv_append_paged_minmax", mk, mv, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots)
+
+
+def ecco_kv_attend_paged_workspace(n_tokens: int, B: int, Hq: int, Hkv: int, max_new: int, max_kv: int, total_kv: int, device: int = 0) -> int:
+    """Bytes of the workspace that ecco_kv_attend_paged needs for these sizes."""
+    return int(lib().ecco_kv_attend_paged_workspace(device, n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv))
+
+
+def ecco_kv_attend_paged(mk: Model, mv: Model, q, k_blocks, k_meta, v_blocks, v_meta, page_table, q_start, kv_len, max_new: int, max_kv: int,
+                         total_kv: int | None = None, workspace=None, out=None):
+    """q: CUDA FP16 [n_tokens, Hq, 128], a view into a wider tensor allowed; out: FP32 (the default) or FP16 [n_tokens, Hq, 128].  max_new,
+    max_kv: at least the most new tokens and the most tokens of a sequence; total_kv: at least the tokens of all of them (default: B times
+    max_kv); workspace: uint8 tensor of ecco_kv_attend_paged_workspace bytes."""
+    import torch
+    n_pages, Hkv, page_tokens = _pool(k_blocks, k_meta, v_blocks, v_meta)
+    B, max_pages = page_table.shape
+    n_tokens, Hq = q.shape[:2]
+    total_kv = B * max_kv if total_kv is None else total_kv
+    _int32(page_table, q_start, kv_len)
+    assert q_start.numel() >= B + 1 and kv_len.numel() >= B
+    if out is None:
+        out = torch.empty((n_tokens, Hq, GROUP), dtype=torch.float32, device=q.device)
+    assert out.shape == q.shape and out.dtype in (torch.float32, torch.float16)
+    if workspace is None:
+        size = ecco_kv_attend_paged_workspace(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv, q.device.index or 0)
+        workspace = torch.empty((size,), dtype=torch.uint8, device=q.device) if size else None
+    ptr, stride = _rows(q)
+    _check(lib().ecco_kv_attend_paged(mk.handle, mv.handle, ptr, stride, _dp(k_blocks), _dp(k_meta), _dp(v_blocks), _dp(v_meta), _dp(page_table),
+                                      _dp(q_start), _dp(kv_len), n_tokens, B, Hq, Hkv, n_pages, page_tokens, max_pages, max_new, max_kv, total_kv,
+                                      _dp(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _dp(out),
+                                      int(out.dtype == torch.float16), _stream()), "ecco_kv_attend_paged")
+    return out
 
 
 # ---- the self-contained block format (include/ecco_paper_block.h) ------------------------------------------------

@@ -7,6 +7,7 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <type_traits>
 
 #include "ecco_internal.h"
 #include "ecco_plan.h"
@@ -19,6 +20,7 @@ constexpr int kHalf = kGroup / 2;         // values per chain
 
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float half_bits_f(uint32_t bits) { return __half2float(__ushort_as_half((unsigned short)bits)); }
 
@@ -335,5 +337,51 @@ __device__ __forceinline__ void store_unit(uint32_t* wbuf, const UnitLoad& u, in
     wave_lds_fence();
 }
 
+
+// The merge of n_splits partial results of one query head, a dimension per thread: ml holds their (maximum, denominator) pairs, part this
+// dimension's unnormalised outputs, kGroup apart.
+__device__ __forceinline__ float merge_splits(const float* __restrict__ ml, const float* __restrict__ part, int n_splits) {
+    // Sixteen splits at a time (four or eight where there are no more) with all their loads in flight together, indices
+    // clamped; the additions run in split order.  An empty split (maximum -inf, zeros) gets weight 0, also when every
+    // split is empty (mx = -inf).  The kernel is bound by the latency of the partial results, which come from memory: up to
+    // sixteen splits the maximum is formed from the values in hand and not in a round trip of its own.
+    float num = 0.0f, den = 0.0f;
+    const auto batch = [&](auto count, int s0, float mx) {
+        constexpr int kCount = decltype(count)::value;
+        float m[kCount], d[kCount], v[kCount];
+#pragma unroll
+        for (int j = 0; j < kCount; ++j) {
+            const int sj = min(s0 + j, n_splits - 1);
+            m[j] = ml[2 * sj];
+            d[j] = ml[2 * sj + 1];
+            v[j] = part[(size_t)sj * kGroup];
+        }
+        if (s0 == 0 && n_splits <= kCount) {
+            mx = m[0];
+#pragma unroll
+            for (int j = 1; j < kCount; ++j) mx = fmaxf(mx, m[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kCount; ++j) {
+            if (s0 + j < n_splits) {  // uniform
+                const float w = m[j] == -INFINITY ? 0.0f : __expf(m[j] - mx);
+                num += w * v[j];
+                den += w * d[j];
+            }
+        }
+    };
+    if (n_splits <= 4) batch(std::integral_constant<int, 4>{}, 0, 0.0f);
+    else if (n_splits <= 8) batch(std::integral_constant<int, 8>{}, 0, 0.0f);
+    else if (n_splits <= 16) batch(std::integral_constant<int, 16>{}, 0, 0.0f);
+    else {
+        // the largest of the splits' maxima: a few splits per lane and a wavefront maximum (exact whatever the order),
+        // instead of a chain of n_splits dependent loads
+        float mx = -INFINITY;
+        for (int s = threadIdx.x & 63; s < n_splits; s += 64) mx = fmaxf(mx, ml[2 * s]);
+        mx = wave_all(mx, [](float a, float b) { return fmaxf(a, b); });
+        for (int s0 = 0; s0 < n_splits; s0 += 16) batch(std::integral_constant<int, 16>{}, s0, mx);
+    }
+    return den > 0.0f ? num / den : 0.0f;
+}
 
 }  // namespace ecco_chain

@@ -1,5 +1,5 @@
 // Encoders of the two-chain block format for gfx950: bulk (ecco_encode, ecco_encode_minmax) and appended tokens
-// (ecco_kv_append, ecco_kv_append_minmax).
+// (ecco_kv_append, ecco_kv_append_minmax; into pages ecco_kv_append_paged, ecco_kv_append_paged_minmax).
 //
 // What bounds them.  Rating all S patterns value by value is 24 vector instructions per value and pattern for 16
 // candidates: 48 wavefront instructions per group and pattern, 4 ns per group on the whole chip at S = 64, where reading
@@ -14,6 +14,8 @@
 #include <type_traits>
 
 #include "ecco_launch.h"
+#include "ecco_paged.h"
+#include "ecco_plan.h"
 #include "ecco_rows.h"
 #include "ecco_stream.h"
 
@@ -57,6 +59,36 @@ struct AppendIo {
         return t >= 0 && t < t_max;
     }
 };
+// rows of new tokens: group (row, h) goes to the row's slot in head h of its page, if the slot is one of the pool's
+struct PagedIo {
+    static constexpr bool kDense = false;
+    const uint32_t* src;
+    uint32_t* blocks;
+    uint32_t* meta;
+    const int32_t* slots;
+    int64_t stride;  // words from row to row
+    int n, heads, shift;
+    uint32_t n_slots;
+    __device__ __forceinline__ size_t groups() const { return (size_t)n; }
+    __device__ __forceinline__ bool place(size_t i, size_t& at) const {
+        if (i >= (size_t)n) return false;
+        const uint32_t row = (uint32_t)i / (uint32_t)heads, h = (uint32_t)i - row * (uint32_t)heads, slot = (uint32_t)slots[row];
+        at = (((size_t)(slot >> shift) * heads + h) << shift) + (slot & ((1u << shift) - 1u));
+        return slot < n_slots;
+    }
+    template <int kBatch>
+    __device__ __forceinline__ void load(RowValues& v, size_t b, int local, int l) const {
+        const uint32_t i = (uint32_t)min(b * kBatch + (uint32_t)local, (size_t)(n - 1)), row = i / (uint32_t)heads, h = i - row * (uint32_t)heads;
+        const u32x4_dword t = *reinterpret_cast<const u32x4_dword*>(src + (size_t)row * stride + (h * kRowLanes + l) * 4);
+        v.x[0] = t.x; v.x[1] = t.y; v.x[2] = t.z; v.x[3] = t.w;
+    }
+};
+// the values of group `local` of batch b
+template <int kBatch, class Io>
+__device__ __forceinline__ void load_group(RowValues& v, const Io& io, size_t b, int local, int l) {
+    if constexpr (std::is_same<Io, PagedIo>::value) io.template load<kBatch>(v, b, local, l);
+    else load_values<kBatch>(v, io.values(), io.groups(), b, local, l);
+}
 template <class Io>
 struct Job {  // one model and the groups it encodes; blockIdx.y picks one of two (keys and values)
     const uint32_t* dev;
@@ -181,7 +213,7 @@ __global__ __launch_bounds__(kSearchThreads) __attribute__((amdgpu_waves_per_eu(
     uint32_t* hist = L.hist + (wave * kWaveRows + row) * kHistStride;
     const size_t batches = (io.groups() + kSearchBatch - 1) / kSearchBatch;
     RowValues v;
-    load_values<kSearchBatch>(v, io.values(), io.groups(), blockIdx.x, wave * kWaveRows + row, l);
+    load_group<kSearchBatch>(v, io, blockIdx.x, wave * kWaveRows + row, l);
     Coefs<kTiles> C;
     C.load(job.dev + DevLayout{S}.coef(), wave, tiles, lane);
     const EncTables T = stage_enc_tables<kSearchThreads, false>(smem, job.dev, S);
@@ -263,7 +295,7 @@ __global__ __launch_bounds__(kSearchThreads) __attribute__((amdgpu_waves_per_eu(
         int last = threadIdx.x & 63;  // the lane taken afresh: what is derived from it is formed here, not kept through the search
         asm volatile("" : "+v"(last));
         const int place = last & 15, group = wave * kWaveRows + (last >> 4);
-        load_values<kSearchBatch>(v, io.values(), io.groups(), b + gridDim.x, group, place);
+        load_group<kSearchBatch>(v, io, b + gridDim.x, group, place);
         uint32_t mw;
         const uint32_t word = pack_row<kLong>(T.enc + pattern * (kK * 4u), L.hist + group * kHistStride, idx, place, smax, pattern, mw);
         size_t at;
@@ -348,7 +380,7 @@ __global__ __launch_bounds__(kFewThreads) void encode_few_kernel(Job<Io> j0, Job
     size_t at;
     if (!io.place(g, at)) return;  // uniform
     RowValues v;
-    load_values<1>(v, io.values(), io.groups(), g, 0, l);
+    load_group<1>(v, io, g, 0, l);
     static_assert(kMaxS * kK / 4 <= kFewThreads, "a piece of each table per thread");
     {
         const DevLayout D{S};
@@ -479,7 +511,7 @@ __global__ __launch_bounds__(kMinmaxThreads) void encode_minmax_kernel(Job<Io> j
     uint32_t* image = ends + S + (wave * kWaveRows + row) * kImageStride;
     const size_t batches = (io.groups() + kMinmaxBatch - 1) / kMinmaxBatch;
     RowValues v, next;
-    load_values<kMinmaxBatch>(v, io.values(), io.groups(), blockIdx.x, wave * kWaveRows + row, l);
+    load_group<kMinmaxBatch>(v, io, blockIdx.x, wave * kWaveRows + row, l);
     const EncTables T = stage_enc_tables<kMinmaxThreads, kFine>(smem, job.dev, S);
     if ((int)threadIdx.x < S) {
         const uint32_t* pair = job.dev + DevLayout{S}.pair() + threadIdx.x * 16;
@@ -488,7 +520,7 @@ __global__ __launch_bounds__(kMinmaxThreads) void encode_minmax_kernel(Job<Io> j
     __syncthreads();
     for (size_t b = blockIdx.x; b < batches; b += gridDim.x) {
         const size_t g = b * kMinmaxBatch + wave * kWaveRows + row;
-        load_values<kMinmaxBatch>(next, io.values(), io.groups(), b + gridDim.x, wave * kWaveRows + row, l);
+        load_group<kMinmaxBatch>(next, io, b + gridDim.x, wave * kWaveRows + row, l);
         const half2_t ends2 = row_ends(v);
         const uint32_t both = __builtin_bit_cast(uint32_t, ends2) & 0x7FFF7FFFu, smax = max(both & 0xFFFFu, both >> 16);
         const float s = half_bits_f(smax);
@@ -600,6 +632,26 @@ int kv_append_common(bool minmax, const ecco_model* mk, const ecco_model* mv, co
     return launch_encode(minmax, mk, k, mv, v, (size_t)B * H, 2, stream);
 }
 
+int kv_append_paged_common(bool minmax, const ecco_model* mk, const ecco_model* mv, const uint16_t* k_new, const uint16_t* v_new, int64_t k_stride, int64_t v_stride,
+                           void* k_blocks, uint32_t* k_meta, void* v_blocks, uint32_t* v_meta,
+                           const int32_t* slots, int n_tokens, int H, int n_pages, int page_tokens, void* stream) {
+    if (!mk || !mv) return ECCO_EINVAL;
+    if (n_tokens != 0 && (!k_new || !v_new || !k_blocks || !k_meta || !v_blocks || !v_meta || !slots)) return ECCO_EINVAL;
+    if (n_tokens < 0 || H <= 0 || !pool_fits(page_tokens, n_pages) || (long long)n_tokens * H > 0x7FFFFFFF) return ECCO_ESHAPE;
+    for (const int64_t stride : {k_stride, v_stride})
+        if (stride < (int64_t)H * kGroup || stride % 2 != 0 || stride > ((int64_t)1 << 40)) return ECCO_ESHAPE;
+    if (!aligned(k_blocks, 64) || !aligned(v_blocks, 64)) return ECCO_EALIGN;
+    for (const void* p : {(const void*)k_new, (const void*)v_new, (const void*)k_meta, (const void*)v_meta, (const void*)slots})
+        if (!aligned(p, 4)) return ECCO_EALIGN;
+    if (model_ready(mk) != ECCO_OK || model_ready(mv) != ECCO_OK || mk->device != mv->device) return ECCO_EINVAL;
+    if (n_tokens == 0) return ECCO_OK;
+    const int shift = __builtin_ctz((unsigned)page_tokens);
+    const uint32_t n_slots = (uint32_t)n_pages << shift;
+    const PagedIo k{reinterpret_cast<const uint32_t*>(k_new), static_cast<uint32_t*>(k_blocks), k_meta, slots, k_stride / 2, n_tokens * H, H, shift, n_slots};
+    const PagedIo v{reinterpret_cast<const uint32_t*>(v_new), static_cast<uint32_t*>(v_blocks), v_meta, slots, v_stride / 2, n_tokens * H, H, shift, n_slots};
+    return launch_encode(minmax, mk, k, mv, v, (size_t)n_tokens * H, 2, stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -622,6 +674,18 @@ int ecco_kv_append_minmax(const ecco_model* mk, const ecco_model* mv, const uint
                           void* k_blocks, uint32_t* k_meta, void* v_blocks, uint32_t* v_meta,
                           const int32_t* seq_len, int B, int H, int T_max, void* stream) {
     return kv_append_common(true, mk, mv, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, seq_len, B, H, T_max, stream);
+}
+
+int ecco_kv_append_paged(const ecco_model* mk, const ecco_model* mv, const uint16_t* k_new, const uint16_t* v_new, int64_t k_stride, int64_t v_stride,
+                         void* k_blocks, uint32_t* k_meta, void* v_blocks, uint32_t* v_meta,
+                         const int32_t* slots, int n_tokens, int H, int n_pages, int page_tokens, void* stream) {
+    return kv_append_paged_common(false, mk, mv, k_new, v_new, k_stride, v_stride, k_blocks, k_meta, v_blocks, v_meta, slots, n_tokens, H, n_pages, page_tokens, stream);
+}
+
+int ecco_kv_append_paged_minmax(const ecco_model* mk, const ecco_model* mv, const uint16_t* k_new, const uint16_t* v_new, int64_t k_stride, int64_t v_stride,
+                                void* k_blocks, uint32_t* k_meta, void* v_blocks, uint32_t* v_meta,
+                                const int32_t* slots, int n_tokens, int H, int n_pages, int page_tokens, void* stream) {
+    return kv_append_paged_common(true, mk, mv, k_new, v_new, k_stride, v_stride, k_blocks, k_meta, v_blocks, v_meta, slots, n_tokens, H, n_pages, page_tokens, stream);
 }
 
 }  // extern "C"

@@ -311,7 +311,6 @@ __global__ __launch_bounds__(kDecWaves * 64) void decode_kernel(const uint32_t* 
 // block the 16 wavefronts add their accumulators through LDS in a fixed order.
 constexpr int kMmaRows = 16;
 constexpr int kMaxBatch = 16;
-typedef float float4_t __attribute__((ext_vector_type(4)));
 constexpr int kRbChunk = 3;  // row blocks whose per-wavefront sums wait in LDS for one common reduction
 static_assert((table_words(ECCO_MAX_S) + (size_t)(kGemvThreads / 64) * (32 * kStride + 4) + (size_t)kRbChunk * (kGemvThreads / 64) * 16 * 16) * 4 <= 160 * 1024, "the batched kernel's LDS fits a compute unit");
 inline size_t gemm_lds_bytes(int S) { return (table_words(S) + (size_t)kWaves * kUnitWords + (size_t)kRbChunk * kWaves * kMmaRows * kMaxBatch) * 4; }
@@ -974,47 +973,7 @@ __global__ __launch_bounds__(kGroup) void kv_attend_combine_kernel(const float* 
     const size_t bh = blockIdx.x;
     const float* ml = ws + (size_t)n_heads * n_splits * kGroup + bh * n_splits * 2;
     const float* part = ws + bh * n_splits * kGroup + threadIdx.x;
-    // Sixteen splits at a time (four or eight where there are no more) with all their loads in flight together, indices
-    // clamped; the additions run in split order.  An empty split (maximum -inf, zeros) gets weight 0, also when every
-    // split is empty (mx = -inf).  The kernel is bound by the latency of the partial results, which come from memory: up to
-    // sixteen splits the maximum is formed from the values in hand and not in a round trip of its own.
-    float num = 0.0f, den = 0.0f;
-    const auto batch = [&](auto count, int s0, float mx) {
-        constexpr int kCount = decltype(count)::value;
-        float m[kCount], d[kCount], v[kCount];
-#pragma unroll
-        for (int j = 0; j < kCount; ++j) {
-            const int sj = min(s0 + j, n_splits - 1);
-            m[j] = ml[2 * sj];
-            d[j] = ml[2 * sj + 1];
-            v[j] = part[(size_t)sj * kGroup];
-        }
-        if (s0 == 0 && n_splits <= kCount) {
-            mx = m[0];
-#pragma unroll
-            for (int j = 1; j < kCount; ++j) mx = fmaxf(mx, m[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < kCount; ++j) {
-            if (s0 + j < n_splits) {  // uniform
-                const float w = m[j] == -INFINITY ? 0.0f : __expf(m[j] - mx);
-                num += w * v[j];
-                den += w * d[j];
-            }
-        }
-    };
-    if (n_splits <= 4) batch(std::integral_constant<int, 4>{}, 0, 0.0f);
-    else if (n_splits <= 8) batch(std::integral_constant<int, 8>{}, 0, 0.0f);
-    else if (n_splits <= 16) batch(std::integral_constant<int, 16>{}, 0, 0.0f);
-    else {
-        // the largest of the splits' maxima: a few splits per lane and a wavefront maximum (exact whatever the order),
-        // instead of a chain of n_splits dependent loads
-        float mx = -INFINITY;
-        for (int s = threadIdx.x & 63; s < n_splits; s += 64) mx = fmaxf(mx, ml[2 * s]);
-        mx = wave_all(mx, [](float a, float b) { return fmaxf(a, b); });
-        for (int s0 = 0; s0 < n_splits; s0 += 16) batch(std::integral_constant<int, 16>{}, s0, mx);
-    }
-    out[bh * kGroup + threadIdx.x] = den > 0.0f ? num / den : 0.0f;
+    out[bh * kGroup + threadIdx.x] = merge_splits(ml, part, n_splits);
 }
 
 // ---- device scratch of the entry point that allocates nothing -----------------------------------------------

@@ -1,0 +1,494 @@
+// Attention of a step's new tokens over the paged compressed cache (include/ecco_paged.h).
+#include <hip/hip_runtime.h>
+#include <hip/hip_fp16.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "ecco_decode.h"
+#include "ecco_launch.h"
+#include "ecco_paged.h"
+#include "ecco_plan.h"
+
+using namespace ecco;
+using namespace ecco_chain;
+
+namespace {
+
+struct PagedArgs {
+    const uint32_t* dev_k;
+    const uint32_t* dev_v;
+    const uint16_t* q;
+    const uint4* k_blocks;
+    const uint32_t* k_meta;
+    const uint4* v_blocks;
+    const uint32_t* v_meta;
+    const int32_t* table;
+    const int32_t* q_start;
+    const int32_t* kv_len;
+    void* out;
+    float* ws;
+    int64_t q_stride;
+    int Sk, Sv, B, Hq, Hkv, n_tokens, n_pages, shift, max_pages, max_kv;
+    int tiles, table_words, both, span, step, half;
+};
+
+// The arguments of the running kernel, read again: what the loops need of them once per unit would otherwise take scalar registers
+// throughout, and those are short beside the decoders.
+typedef const __attribute__((address_space(4))) PagedArgs args_t;
+__device__ __forceinline__ args_t* fresh_args() {
+    args_t* a = (args_t*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(a));
+    return a;
+}
+template <class T>
+__device__ __forceinline__ const __attribute__((address_space(1))) T* in_global(const T* p) { return (const __attribute__((address_space(1))) T*)p; }
+
+__device__ __forceinline__ void store_out(args_t* a, size_t at, float v) {
+    if (a->half) ((__attribute__((address_space(1))) _Float16*)a->out)[at] = (_Float16)v;
+    else ((__attribute__((address_space(1))) float*)a->out)[at] = v;
+}
+// (a pointer that is read back is known to be global memory only by a cast there and back)
+__device__ __forceinline__ const uint32_t* global_words(const uint32_t* p) { return (const uint32_t*)in_global(p); }
+
+// What the lengths of the device say of sequence b, within what the host has sized the launch for (no rows if they are none of q's)
+struct Sequence {
+    int row0, n_new, kv;  // first row, rows, tokens to read
+    __device__ __forceinline__ Sequence(args_t* a, int b) {
+        const auto* start = in_global(a->q_start);
+        row0 = start[b];
+        const int end = start[b + 1];
+        n_new = row0 >= 0 && end <= a->n_tokens ? max(0, end - row0) : 0;
+        kv = max(0, min(in_global(a->kv_len)[b], a->max_kv));
+    }
+};
+
+// The pages that hold the two halves of a unit of 32 tokens (a page has 16 tokens at least).  The same for all lanes, but in vector
+// registers.
+struct UnitPages {
+    int page[2];
+};
+__device__ __forceinline__ bool in_pool(int page, int n_pages) { return (uint32_t)page < (uint32_t)n_pages; }
+// of the unit that begins at token t0 of sequence b; `last`: the last token that is read of it
+__device__ __forceinline__ UnitPages unit_pages(int b, int t0, int last) {
+    args_t* a = fresh_args();
+    int zero = 0;
+    asm volatile("" : "+v"(zero));
+    const auto* row = in_global(a->table) + (size_t)b * a->max_pages;
+    UnitPages p;
+    p.page[0] = row[(min(t0, last) >> a->shift) + zero];
+    p.page[1] = row[(min(t0 + kUnitBlocks / 2, last) >> a->shift) + zero];
+    return p;
+}
+// As load_unit of the contiguous caches: the payload pieces of this lane and the meta word of the unit's block `tok`, which it decodes (tokens
+// 16 on belong to lanes 32 on).  Slots of a page are all readable, whether they hold a token or not; of a page that is none the first one's are read.
+// ok: whether the page of token `tok` is one
+template <bool kValues>
+__device__ __forceinline__ UnitLoad load_unit(const UnitPages& p, int hkv, int t0, int lane, int tok, bool& ok) {
+    args_t* a = fresh_args();
+    const uint32_t mask = (1u << a->shift) - 1u;
+    size_t at[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        at[h] = (((size_t)(uint32_t)(in_pool(p.page[h], a->n_pages) ? p.page[h] : 0) * (uint32_t)a->Hkv + (uint32_t)hkv) << a->shift) + (((uint32_t)t0 + 16u * h) & mask);
+    const global_u4* blocks = (const global_u4*)(kValues ? a->v_blocks : a->k_blocks);
+    const auto* meta = in_global(kValues ? a->v_meta : a->k_meta);
+    const u32x4 v0 = blocks[at[0] * 4 + lane], v1 = blocks[at[1] * 4 + lane];
+    UnitLoad u;
+    u.v0 = make_uint4(v0.x, v0.y, v0.z, v0.w);
+    u.v1 = make_uint4(v1.x, v1.y, v1.z, v1.w);
+    u.meta = meta[(lane < 32 ? at[0] : at[1]) + (tok & 15)];
+    ok = in_pool(lane < 32 ? p.page[0] : p.page[1], a->n_pages);
+    return u;
+}
+
+// ---- few rows per key/value head ---------------------------------------------------------------------------------------
+// The rows of a sequence and a key/value head are its new tokens times the grp = Hq / Hkv query heads that share it, row r being head r % grp of
+// new token r / grp.  A workgroup takes up to 16 of them over a range of the sequence's tokens, and decodes every K and V block of the range on
+// the way into the products, as the grouped-query kernel over contiguous caches does (kv_attend_gqa_kernel says how tiles, halves and rests lie; the
+// columns here are rows in this sense, each with an end of its own: what a token sees ends with itself).
+// grid: (B * Hkv, n_splits, tiles of 16 rows).  The partial result of a split and row is at index ((sequence and head * tiles + tile) * 16
+// + row) * n_splits + split of the workspace: 128 outputs each, then (maximum, denominator) pairs.
+template <bool kLongK, bool kLongV, bool kWide, int kWaves>
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWaves == 12 ? 3 : 4))) void attend_rows_kernel(PagedArgs) {
+    constexpr int kThreads = kWaves * 64;
+    static_assert(2 * kThreads >= kMaxS * kK, "load_table_items: two table items per thread cover every model");
+    constexpr int kOutputs = (kGqaMaxGroup * kGroup + kThreads - 1) / kThreads;  // output elements per thread
+    args_t* const first = fresh_args();
+    const int both = first->both, table_words = first->table_words, Hkv = first->Hkv;
+    extern __shared__ __align__(16) uint32_t smem[];
+    const int grp = first->Hq / Hkv, sstride = gqa_score_stride(first->span);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int b = blockIdx.x / Hkv, hkv = blockIdx.x - b * Hkv, split = blockIdx.y, row_begin = blockIdx.z * kGqaMaxGroup;
+    const Sequence seq(first, b);
+    const int rows = min(kGqaMaxGroup, seq.n_new * grp - row_begin);
+    if (rows <= 0) return;  // uniform, ahead of every barrier
+    float* state = reinterpret_cast<float*>(smem);  // [wavefront][16] maxima, [wavefront][16] denominators
+    uint32_t* k_tables = smem + gqa_state_words(kWaves);
+    uint32_t* wbuf = k_tables + table_words + wave * kUnitWords;
+    uint32_t* tile = k_tables + table_words + kWaves * kUnitWords + wave * kTileWords;
+    float* scores = reinterpret_cast<float*>(k_tables + table_words + kWaves * (kUnitWords + kTileWords));  // [rows][sstride]
+    uint32_t* v_tables = k_tables + (both ? decode_table_words(first->Sk, kLongK) : 0);
+    if (lane < kUnitBlocks) wbuf[lane * kStride + kBlockWords] = 0u;
+
+    // the last row's token sees the most: T tokens
+    const int T = max(0, seq.kv - seq.n_new + (row_begin + rows - 1) / grp + 1), last = T - 1;
+    const int n_splits = gridDim.y;
+    const int64_t per_range = (int64_t)((units_of(max(T, 1)) + n_splits - 1) / n_splits) * kUnitBlocks;
+    const int t_begin = (int)min((int64_t)T, split * per_range), t_end = (int)min((int64_t)T, (split + 1) * per_range);
+    const int span_max = t_end - t_begin <= first->span ? first->span : first->step;  // a range that one span holds is not cut
+    struct Place {
+        int lane, n, slice, half, tok;  // n: matrix-core row or column; slice: k slice; half: chain of the lane's token `tok` of the unit
+        __device__ Place() : lane(fresh_thread() & 63), n(lane & 15), slice(lane >> 4), half(slice & 1), tok(n + 16 * (lane >> 5)) {}
+    };
+    const float inv_sqrt_d = 0.08838834764831845f;  // 1 / sqrt(128)
+    float4_t o[8];  // tile j: row r is dimension 64 (r / 8) + 8 j + r % 8, column the row
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    float run_max = -INFINITY, run_den = 0.0f;  // of this wavefront and of row l % 16; the denominator of the lane's tokens
+
+    for (int s0 = t_begin; s0 < t_end; s0 += span_max) {
+        const int span = min(span_max, t_end - s0);
+        const int units = (span + kUnitBlocks - 1) / kUnitBlocks;  // s0 is a multiple of 32
+        UnitLoad pre;
+        bool pre_ok;
+        UnitPages now, next;  // of the unit that `pre` holds, and of the one behind it
+        const auto pages_at = [&](int u) { return unit_pages(b, s0 + min(u, units - 1) * kUnitBlocks, last); };
+        // ---- scores of the span, all rows
+        float mx = -INFINITY;
+        {
+        const Place P;
+        const int lane = P.lane, n = P.n, slice = P.slice, half = P.half, tok = P.tok;
+        const int row = kWide ? n : n & 7;                              // row of this lane's column
+        const bool row_ok = row < rows, b_ok = row_ok && (kWide || (n >> 3) == (lane >> 5));
+        const int r = row_begin + min(row, rows - 1), token = r / grp;
+        
+        const int sees = min(span, seq.kv - seq.n_new + token + 1 - s0);  // tokens of the span
+        int u = wave;
+        const auto load_k = [&](int at) { pre = load_unit<false>(now, hkv, s0 + min(at, units - 1) * kUnitBlocks, lane, tok, pre_ok); };
+        uint4 bq[kHalf / 8];  // B operands: the query of this lane's row, dimensions 64 * half + 8j .. + 7
+        const auto load_q = [&] {
+            args_t* a = fresh_args();
+            const global_u4* qsrc = (const global_u4*)(a->q + (int64_t)(seq.row0 + token) * a->q_stride + (hkv * grp + r - token * grp) * kGroup + half * kHalf);
+#pragma unroll
+            for (int j = 0; j < kHalf / 8; ++j) {
+                const u32x4 v = qsrc[j];
+                bq[j] = make_uint4(v.x, v.y, v.z, v.w);
+            }
+        };
+        now = pages_at(u);
+        next = pages_at(u + kWaves);
+        if (!both) {
+            args_t* a = fresh_args();
+            const TableItems items = load_table_items(global_words(a->dev_k), a->Sk);
+            load_k(u);
+            load_q();
+            __syncthreads();  // the V tables of the span before have been read
+            a = fresh_args();
+            build_tables<kLongK>(k_tables, global_words(a->dev_k), a->Sk, items);
+            __syncthreads();
+        } else if (s0 == t_begin) {  // both models' items, then the payload, then both builds
+            args_t* a = fresh_args();
+            const TableItems k_items = load_table_items(global_words(a->dev_k), a->Sk), v_items = load_table_items(global_words(a->dev_v), a->Sv);
+            load_k(u);
+            load_q();
+            a = fresh_args();
+            build_tables<kLongK>(k_tables, global_words(a->dev_k), a->Sk, k_items);
+            build_tables<kLongV>(v_tables, global_words(a->dev_v), a->Sv, v_items);
+            __syncthreads();
+        } else {
+            load_k(u);
+            load_q();
+        }
+        const int Sk = fresh_args()->Sk;
+        const Tables TK = table_pointers(k_tables, Sk);
+#pragma unroll
+        for (int j = 0; j < kHalf / 8; ++j) bq[j] = b_ok ? bq[j] : make_uint4(0u, 0u, 0u, 0u);
+        for (; u < units; u += kWaves) {
+            store_unit(wbuf, pre, lane);
+            // a slot past the range, or of no page, may hold anything: scale 0, so that its values are zeros (tokens m and 16 + m share a row
+            // of the product, and NaN * 0 would poison it)
+            const uint32_t mw = u * kUnitBlocks + tok < span && pre_ok ? pre.meta : (pre.meta & 0xFFFF0000u);
+            const uint64_t pool = __ballot(pre_ok);  // bits 0 and 32: of the unit's two halves
+            if (u + kWaves < units) {
+                now = next;
+                load_k(u + kWaves);
+                next = pages_at(u + 2 * kWaves);
+            }
+            const Lane L = lane_setup(TK, mw, Sk);
+            const _Float16 sh16 = __builtin_bit_cast(_Float16, (unsigned short)(mw & 0xFFFFu));
+            const half2_t s2 = {sh16, sh16};
+            uint32_t pk[4];
+            float4_t acc[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+            decode_chain<kLongK, kHalf>(wbuf + tok * kStride, half ? L.second_start : 0u, L, [&](int i, uint32_t e) {
+                if ((i & 1) == 0) {
+                    pk[(i >> 1) & 3] = e >> 16;
+                    return;
+                }
+                pk[(i >> 1) & 3] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, pk[(i >> 1) & 3] | (e & 0xFFFF0000u)) * s2);
+                if ((i & 7) != 7) return;
+                const half8_t bv = __builtin_bit_cast(half8_t, bq[i >> 3]);
+                if (kWide) {
+                    const bool low = lane < 32;
+                    const uint4 a0 = make_uint4(low ? pk[0] : 0u, low ? pk[1] : 0u, low ? pk[2] : 0u, low ? pk[3] : 0u);
+                    const uint4 a1 = make_uint4(low ? 0u : pk[0], low ? 0u : pk[1], low ? 0u : pk[2], low ? 0u : pk[3]);
+                    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a0), bv, acc[0], 0, 0, 0);
+                    acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a1), bv, acc[1], 0, 0, 0);
+                } else {
+                    const uint4 av = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+                    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, av), bv, acc[0], 0, 0, 0);
+                }
+            });
+            // accumulator layout of the 16 x 16 tile: register i of lane l is row 4 * (l / 16) + i, column l % 16
+#pragma unroll
+            for (int w = 0; w < (kWide ? 2 : 1); ++w) {
+                const bool upper = kWide ? w != 0 : n >= 8, ok = (upper ? (uint32_t)(pool >> 32) : (uint32_t)pool) != 0u;  // of the unit's tokens
+                const int t0 = u * kUnitBlocks + 4 * slice + (upper ? 16 : 0);
+                float4_t v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[i] = ok && t0 + i < sees ? acc[w][i] * inv_sqrt_d : -INFINITY;
+                    mx = fmaxf(mx, v[i]);
+                }
+                if (row_ok) *reinterpret_cast<float4_t*>(scores + row * sstride + t0) = v;  // for this wavefront alone
+            }
+        }
+        // the wavefront's maximum per row: over the lanes of the column
+        if (!kWide) mx = fmaxf(mx, __shfl_xor(mx, 8));
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        }
+        // ---- weighted sum of V over the span
+        const Place P;
+        const int lane = P.lane, n = P.n, slice = P.slice, half = P.half, tok = P.tok;
+        const uint32_t swap_sel = (lane & 1) ? 0x03020706u : 0x05040100u;  // odd lanes keep the high halves, even lanes the low halves
+        int u = wave;
+        const auto load_v = [&](int at) { pre = load_unit<true>(now, hkv, s0 + min(at, units - 1) * kUnitBlocks, lane, tok, pre_ok); };
+        now = pages_at(u);
+        next = pages_at(u + kWaves);
+        if (both) {
+            load_v(u);
+        } else {
+            args_t* a = fresh_args();
+            const TableItems items = load_table_items(global_words(a->dev_v), a->Sv);
+            load_v(u);
+            __syncthreads();
+            a = fresh_args();
+            build_tables<kLongV>(v_tables, global_words(a->dev_v), a->Sv, items);
+            __syncthreads();
+        }
+        const int Sv = fresh_args()->Sv;
+        const Tables TV = table_pointers(v_tables, Sv);
+        const float before = run_max;
+        run_max = fmaxf(before, mx);
+        const float base = run_max == -INFINITY ? 0.0f : run_max;  // (a wavefront without units, or without a score above -inf)
+        if (s0 != t_begin) {  // every accumulator of a lane belongs to row l % 16
+            const float alpha = before == -INFINITY ? 0.0f : __expf(before - base);
+            run_den *= alpha;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] *= alpha;
+        }
+        const int row = kWide ? n : n & 7;
+        const float* score = scores + min(row, rows - 1) * sstride + 8 * slice;
+        for (; u < units; u += kWaves) {
+            store_unit(wbuf, pre, lane);
+            const uint32_t mw = u * kUnitBlocks + tok < span && pre_ok ? pre.meta : (pre.meta & 0xFFFF0000u);
+            if (u + kWaves < units) {
+                now = next;
+                load_v(u + kWaves);
+                next = pages_at(u + 2 * kWaves);
+            }
+            const Lane L = lane_setup(TV, mw, Sv);
+            const _Float16 sh16 = __builtin_bit_cast(_Float16, (unsigned short)(mw & 0xFFFFu));
+            const half2_t s2 = {sh16, sh16};
+            // B operand: probabilities of row l % 16 for tokens 8 * (l / 16) .. + 7 of the unit, 0 for what is not seen.  What an
+            // FP16 probability leaves of the FP32 one is the operand of a product of its own, or with up to eight rows of columns 8..15.
+            const float taken = !kWide && n < 8 ? 0.0f : 1.0f;
+            half8_t pb, rest;
+            {
+                const float4_t s[2] = {reinterpret_cast<const float4_t*>(score + u * kUnitBlocks)[0], reinterpret_cast<const float4_t*>(score + u * kUnitBlocks)[1]};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float p = row < rows ? __expf(s[i >> 2][i & 3] - base) : 0.0f;
+                    pb[i] = (_Float16)p;
+                    rest[i] = (_Float16)fmaf(-taken, (float)pb[i], p);
+                    run_den += p;
+                }
+                if (!kWide) pb = rest;
+            }
+            uint32_t pk[4];
+            decode_chain<kLongV, kHalf>(wbuf + tok * kStride, half ? L.second_start : 0u, L, [&](int i, uint32_t e) {
+                if ((i & 1) == 0) {
+                    pk[(i >> 1) & 3] = e >> 16;
+                    return;
+                }
+                pk[(i >> 1) & 3] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, pk[(i >> 1) & 3] | (e & 0xFFFF0000u)) * s2);
+                if ((i & 7) != 7) return;
+                // 8 values of this lane's token -> rows 8 * half + r of the tile (dimension 64 * half + 8 * (i / 8) + r);
+                // an even lane takes dimension 2 r2 of its own and its neighbour's token, the odd neighbour dimension 2 r2 + 1
+                wave_lds_fence();
+#pragma unroll
+                for (int r2 = 0; r2 < 4; ++r2) {
+                    const uint32_t other = (uint32_t)__builtin_amdgcn_mov_dpp((int)pk[r2], 0xB1, 0xF, 0xF, true);  // quad_perm [1,0,3,2]
+                    tile[(8 * half + 2 * r2 + (lane & 1)) * kTileStride + (tok >> 1)] = __builtin_amdgcn_perm(other, pk[r2], swap_sel);
+                }
+                wave_lds_fence();
+                const uint4 a0 = *reinterpret_cast<const uint4*>(tile + n * kTileStride + 4 * slice);
+                o[i >> 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a0), pb, o[i >> 3], 0, 0, 0);
+                if (kWide) o[i >> 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a0), rest, o[i >> 3], 0, 0, 0);
+            });
+        }
+    }
+    // ---- sum over the wavefronts; everything in LDS but the state is dead behind the first barrier
+    const Place P;
+    const int n = P.n, slice = P.slice;
+    args_t* const a = fresh_args();
+    float* const ws = a->ws;
+    const int n_tiles = a->tiles;
+    const size_t part = ((size_t)blockIdx.x * n_tiles + blockIdx.z) * kGqaMaxGroup * n_splits + split;  // of the tile's first row
+    const size_t total = (size_t)gridDim.x * n_tiles * kGqaMaxGroup * n_splits;
+    run_den += __shfl_xor(run_den, 16);
+    run_den += __shfl_xor(run_den, 32);
+    if (lane < 16) state[wave * kGqaMaxGroup + lane] = run_max;
+    __syncthreads();
+    float most = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) most = fmaxf(most, state[w * kGqaMaxGroup + n]);
+    const float mine = run_max == -INFINITY ? 0.0f : __expf(run_max - most);
+    if (lane < 16) state[(kWaves + wave) * kGqaMaxGroup + lane] = run_den * mine;
+    float* red = reinterpret_cast<float*>(k_tables);  // [wavefront][8 tiles][4 slices][16 lanes][4]
+    if (!kWide) {  // what the rests contributed
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float here = o[j][i];
+                o[j][i] = here + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, here), 0x128, 0xF, 0xF, true));  // row_ror:8
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) *reinterpret_cast<float4_t*>(red + (wave * 8 + j) * kRedTile + slice * kRedRow + n * 4) = o[j] * mine;
+    __syncthreads();
+    const auto denominator = [&](int g) {
+        float den = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) den += state[(kWaves + w) * kGqaMaxGroup + g];
+        return den;
+    };
+    if (n_splits > 1 && tid < rows) {  // (the first wavefront's lane of row `tid` holds that row's maximum)
+        const size_t at = total * kGroup + (part + (size_t)tid * n_splits) * 2;
+        ws[at] = most;
+        ws[at + 1] = denominator(tid);
+    }
+#pragma unroll
+    for (int k = 0; k < kOutputs; ++k) {
+        const int e = tid + k * kThreads, g = e / kGroup, dim = e % kGroup;
+        if (g < rows) {
+            const int at_row = 8 * (dim >> 6) + (dim & 7);
+            const float* at = red + ((dim & 63) >> 3) * kRedTile + (at_row >> 2) * kRedRow + g * 4 + (at_row & 3);
+            float sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) sum += at[w * 8 * kRedTile];
+            if (n_splits == 1) {
+                const float den = denominator(g);
+                const int r = row_begin + g, token = r / grp;
+                store_out(a, ((size_t)(seq.row0 + token) * a->Hq + hkv * grp + r - token * grp) * kGroup + dim, den > 0.0f ? sum / den : 0.0f);
+            } else {
+                ws[(part + (size_t)g * n_splits) * kGroup + dim] = sum;
+            }
+        }
+    }
+}
+
+// merges the token ranges of a row: grid (B * Hkv, rows of a tile that there may be, tiles), 128 threads
+__global__ __launch_bounds__(kGroup) void attend_rows_merge_kernel(PagedArgs args, int n_splits) {
+    args_t* const a = fresh_args();
+    const int b = blockIdx.x / args.Hkv, hkv = blockIdx.x - b * args.Hkv, grp = args.Hq / args.Hkv;
+    const Sequence seq(a, b);
+    const int r = blockIdx.z * kGqaMaxGroup + blockIdx.y, token = r / grp;
+    if (r >= seq.n_new * grp) return;
+    const size_t at = (((size_t)blockIdx.x * args.tiles + blockIdx.z) * kGqaMaxGroup + blockIdx.y) * n_splits;
+    const size_t total = (size_t)gridDim.x * args.tiles * kGqaMaxGroup * n_splits;
+    const float v = merge_splits(args.ws + total * kGroup + at * 2, args.ws + at * kGroup + threadIdx.x, n_splits);
+    store_out(a, ((size_t)(seq.row0 + token) * args.Hq + hkv * grp + r - token * grp) * kGroup + threadIdx.x, v);
+}
+
+// ---- host side -----------------------------------------------------------------------------------------------------------
+struct Plan {
+    int tiles, splits;  // of 16 rows; of the tokens
+    size_t bytes;       // of the workspace
+};
+Plan plan_of(int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int cus) {
+    Plan p;
+    const long long rows = (long long)std::min(max_new, n_tokens) * (Hq / Hkv);
+    p.tiles = (int)((rows + kGqaMaxGroup - 1) / kGqaMaxGroup);
+    const long long wgs = (long long)B * Hkv * p.tiles;
+    p.splits = (int)std::min<long long>(std::min<long long>(std::max<long long>(1, cus / wgs), ((long long)max_kv + 255) / 256), 256);
+    p.bytes = p.splits > 1 ? (size_t)wgs * kGqaMaxGroup * p.splits * (kGroup + 2) * sizeof(float) : 0;
+    return p;
+}
+bool sizes_fit(int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv) {
+    return n_tokens >= 0 && B > 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Hq / Hkv <= kGqaMaxGroup && max_new > 0 && max_kv > 0 && total_kv > 0 &&
+           (long long)B * Hkv <= 0x7FFFFFFF && (long long)n_tokens * Hq <= 0x7FFFFFFF;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ecco_kv_attend_paged_workspace(int device, int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv) {
+    if (n_tokens == 0 || !sizes_fit(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv)) return 0;
+    return plan_of(n_tokens, B, Hq, Hkv, max_new, max_kv, cu_count(device)).bytes;
+}
+
+int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint16_t* q, int64_t q_stride,
+                         const void* k_blocks, const uint32_t* k_meta, const void* v_blocks, const uint32_t* v_meta,
+                         const int32_t* page_table, const int32_t* q_start, const int32_t* kv_len,
+                         int n_tokens, int B, int Hq, int Hkv, int n_pages, int page_tokens, int max_pages,
+                         int max_new, int max_kv, int64_t total_kv, void* workspace, size_t workspace_bytes,
+                         void* out, int out_half, void* stream) {
+    if (!mk || !mv) return ECCO_EINVAL;
+    if (n_tokens != 0 && (!q || !k_blocks || !k_meta || !v_blocks || !v_meta || !page_table || !q_start || !kv_len || !out)) return ECCO_EINVAL;
+    if (out_half != 0 && out_half != 1) return ECCO_EINVAL;
+    if (!sizes_fit(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv) || !pool_fits(page_tokens, n_pages) || !pool_fits(page_tokens, max_pages)) return ECCO_ESHAPE;
+    if (q_stride < (int64_t)Hq * kGroup || q_stride % 8 != 0 || q_stride > ((int64_t)1 << 40)) return ECCO_ESHAPE;
+    if (!aligned(k_blocks, 64) || !aligned(v_blocks, 64) || !aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 256)) return ECCO_EALIGN;
+    for (const void* p : {(const void*)k_meta, (const void*)v_meta, (const void*)page_table, (const void*)q_start, (const void*)kv_len})
+        if (!aligned(p, 4)) return ECCO_EALIGN;
+    if (model_ready(mk) != ECCO_OK || model_ready(mv) != ECCO_OK || mk->device != mv->device) return ECCO_EINVAL;
+    if (n_tokens == 0) return ECCO_OK;
+    const int dev_id = mk->device, cus = cu_count(dev_id), shift = __builtin_ctz((unsigned)page_tokens);
+    max_kv = std::min(max_kv, max_pages << shift);
+    const Plan plan = plan_of(n_tokens, B, Hq, Hkv, max_new, max_kv, cus);
+    if (plan.bytes > 0 && (!workspace || workspace_bytes < plan.bytes)) return ECCO_EINVAL;
+    const bool lk = mk->max_len > kPeekBits, lv = mv->max_len > kPeekBits;
+    const int rows = std::min(kGqaMaxGroup, std::min(max_new, n_tokens) * (Hq / Hkv));
+    const int units = (units_of(max_kv) + plan.splits - 1) / plan.splits;
+    const GqaPlan g = gqa_plan(mk->S, lk, mv->S, lv, rows, (size_t)B * Hkv * plan.tiles * plan.splits, units, cus);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const PagedArgs args{mk->dev, mv->dev, q, static_cast<const uint4*>(k_blocks), k_meta, static_cast<const uint4*>(v_blocks), v_meta, page_table, q_start, kv_len,
+                         out, static_cast<float*>(workspace), q_stride, mk->S, mv->S, B, Hq, Hkv, n_tokens, n_pages, shift, max_pages, max_kv,
+                         plan.tiles, g.table_words, g.both, g.span, g.step, out_half};
+    const auto launch = [&](auto kernel) -> int {
+        const int rc = allow_lds(kernel, dev_id, g.lds);
+        if (rc != ECCO_OK) return rc;
+        hipLaunchKernelGGL(kernel, dim3(B * Hkv, plan.splits, plan.tiles), dim3(g.waves * 64), g.lds, st, args);
+        ECCO_HIP_CHECK(hipGetLastError());
+        return ECCO_OK;
+    };
+    const auto pick = [&](auto wide) -> int {
+        constexpr bool kWide = decltype(wide)::value;
+        if (lk) return lv ? launch(attend_rows_kernel<true, true, kWide, 12>) : launch(attend_rows_kernel<true, false, kWide, 12>);
+        if (lv) return launch(attend_rows_kernel<false, true, kWide, 12>);
+        return g.waves == 8 ? launch(attend_rows_kernel<false, false, kWide, 8>) : launch(attend_rows_kernel<false, false, kWide, 12>);
+    };
+    const int rc = rows > 8 ? pick(std::true_type{}) : pick(std::false_type{});
+    if (rc != ECCO_OK || plan.splits == 1) return rc;
+    hipLaunchKernelGGL(attend_rows_merge_kernel, dim3(B * Hkv, rows, plan.tiles), dim3(kGroup), 0, st, args, plan.splits);
+    ECCO_HIP_CHECK(hipGetLastError());
+    return ECCO_OK;
+}
+
+}  // extern "C"

@@ -38,6 +38,13 @@ constexpr int span_tokens(int units) { return std::min(units, kSpanMax / kUnitBl
 // 30.5 -> 20.1; 512 of 2000 97.5 -> 87.7, 79.7 -> 74.0, 49.0 -> 57.9; 1024 of 1000 108.6 -> 88.9, 97.0 -> 75.2, 60.3 -> 34.8.
 inline bool share_units(size_t wgs, int units, int cus) { return wgs > (size_t)cus && (size_t)units * (size_t)cus <= 16 * wgs; }
 
+// ---- pages (include/ecco_paged.h)
+// whether `pages` pages of `page_tokens` tokens are a pool, or a row of a page table, whose tokens an int32 counts
+constexpr int kPageLeast = kUnitBlocks / 2, kPageMost = 1024;
+constexpr bool pool_fits(int page_tokens, int pages) {
+    return page_tokens >= kPageLeast && page_tokens <= kPageMost && (page_tokens & (page_tokens - 1)) == 0 && pages > 0 && (long long)page_tokens * pages <= 0x7FFFFFFF;
+}
+
 // ---- kv_attend_kernel
 // Two workgroups of eight wavefronts share a compute unit where there are workgroups for it and both models' tables fit half its
 // LDS: each decodes while the other builds or sums.  Otherwise one workgroup takes it, of as few wavefronts as take the fewest rounds over the units
