@@ -35,6 +35,9 @@ def _check_kernel_resources(remarks: str, verbose: bool) -> dict:
         m = re.search(r"remark:\s+VGPRs: (\d+)", line)
         if m and name:
             vgprs[name] = int(m.group(1))
+        m = re.search(r"remark:\s+AGPRs: (\d+)", line)
+        if m and name and int(m.group(1)):  # accumulation registers follow the others, which are rounded up to four
+            vgprs[name] = (vgprs[name] + 3) // 4 * 4 + int(m.group(1))
         m = re.search(r"remark:\s+ScratchSize \[bytes/lane\]: (\d+)", line)
         if m and name:
             found += 1

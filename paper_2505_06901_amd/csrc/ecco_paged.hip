@@ -31,6 +31,7 @@ struct PagedArgs {
     int64_t q_stride;
     int Sk, Sv, B, Hq, Hkv, n_tokens, n_pages, shift, max_pages, max_kv;
     int tiles, table_words, both, span, step, half;
+    int few;  // rows of a sequence and key/value head up to which it is taken 16 at a time
 };
 
 // The arguments of the running kernel, read again: what the loops need of them once per unit would otherwise take scalar registers
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
     const int b = blockIdx.x / Hkv, hkv = blockIdx.x - b * Hkv, split = blockIdx.y, row_begin = blockIdx.z * kGqaMaxGroup;
     const Sequence seq(first, b);
     const int rows = min(kGqaMaxGroup, seq.n_new * grp - row_begin);
-    if (rows <= 0) return;  // uniform, ahead of every barrier
+    if (rows <= 0 || seq.n_new * grp > first->few) return;  // uniform, ahead of every barrier
     float* state = reinterpret_cast<float*>(smem);  // [wavefront][16] maxima, [wavefront][16] denominators
     uint32_t* k_tables = smem + gqa_state_words(kWaves);
     uint32_t* wbuf = k_tables + table_words + wave * kUnitWords;
@@ -408,25 +409,361 @@ __global__ __launch_bounds__(kGroup) void attend_rows_merge_kernel(PagedArgs arg
     const int b = blockIdx.x / args.Hkv, hkv = blockIdx.x - b * args.Hkv, grp = args.Hq / args.Hkv;
     const Sequence seq(a, b);
     const int r = blockIdx.z * kGqaMaxGroup + blockIdx.y, token = r / grp;
-    if (r >= seq.n_new * grp) return;
+    if (r >= seq.n_new * grp || seq.n_new * grp > args.few) return;
     const size_t at = (((size_t)blockIdx.x * args.tiles + blockIdx.z) * kGqaMaxGroup + blockIdx.y) * n_splits;
     const size_t total = (size_t)gridDim.x * args.tiles * kGqaMaxGroup * n_splits;
     const float v = merge_splits(args.ws + total * kGroup + at * 2, args.ws + at * kGroup + threadIdx.x, n_splits);
     store_out(a, ((size_t)(seq.row0 + token) * args.Hq + hkv * grp + r - token * grp) * kGroup + threadIdx.x, v);
 }
 
+// ---- many rows per key/value head ----------------------------------------------------------------------------------------
+// Decoding a block costs as much as the products of its 128 values with a few hundred rows, so a sequence with more than kFewRows rows per
+// key/value head is decoded once, into the workspace, and then read by all its rows.  What is written are the operands of
+// v_mfma_f32_32x32x16_f16 in the order in which its lanes take them, a unit of 32 tokens at a time (16 KB):
+//   K   A operands of S[token][row] = sum_dim K[token][dim] q[row][dim]: eight of 1 KB, the s-th for dimensions 16 s .. + 15; lane l takes token
+//       l % 32 and the eight dimensions from 16 s + 8 (l / 32) on
+//   V   A operands of O[dim][row] = sum_token V[token][dim] P[token][row]: the (2 d + s)-th for dimensions 32 d .. + 31 and tokens 16 s .. + 15; lane
+//       l takes dimension 32 d + l % 32 and the tokens 16 s + 4 (l / 32) + (0 1 2 3 8 9 10 11): those whose scores the lane holds after the
+//       first product, so that probabilities become B operands where they are
+// so a unit is copied to LDS as it is, and read from there without bank conflicts.
+constexpr int kFewRows = 2 * kGqaMaxGroup;
+constexpr int kUnitHalves = kUnitBlocks * kGroup;      // FP16 values of a unit's K, or V
+constexpr int kUnitBytes = 2 * kUnitHalves * 2;
+
+// Where sequences lie in the workspace and in the launch: running sums over the sequences
+struct Layout {
+    int32_t* unit_start;  // [B + 1] units of 32 tokens of the sequences with many rows
+    int32_t* tile_start;  // [B + 1] tiles of rows
+    uint32_t* seen;       // [units] a bit per token: whether there is one, on a page of the pool
+    uint4* operands;      // unit u of sequence b and head h at ((unit_start[b] * Hkv + h * units of b) + u) * kUnitBytes
+    float* partial;       // of the splits
+    int units, tiles;     // how many the workspace and the launch hold
+};
+struct TileArgs : PagedArgs {
+    Layout lay;
+    int tile_rows, splits;
+};
+typedef const __attribute__((address_space(4))) TileArgs tile_args_t;
+
+// One wavefront, 64 sequences at a time.  What does not fit the workspace or the launch, by lengths that the host did not announce, gets no tiles.
+__global__ __launch_bounds__(64) void attend_layout_kernel(TileArgs a) {
+    const int lane = threadIdx.x, grp = a.Hq / a.Hkv;
+    int units = 0, tiles = 0;
+    if (lane == 0) a.lay.unit_start[0] = a.lay.tile_start[0] = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        const int b = b0 + lane;
+        int u = 0, t = 0;
+        if (b < a.B) {
+            const Sequence s((args_t*)__builtin_amdgcn_kernarg_segment_ptr(), b);
+            const int rows = s.n_new * grp;
+            if (rows > a.few) {
+                u = s.kv > 0 ? units_of(s.kv) : 0;
+                t = (rows - 1) / a.tile_rows + 1;
+            }
+        }
+        int64_t end_u = u, end_t = t;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t ou = __shfl_up(end_u, d), ot = __shfl_up(end_t, d);
+            end_u += lane >= d ? ou : 0;
+            end_t += lane >= d ? ot : 0;
+        }
+        const bool fits = units + end_u <= a.lay.units && tiles + end_t <= a.lay.tiles;
+        // those that fit are the first ones: sums do not fall
+        const uint64_t good = __ballot(fits);
+        const int last = good == ~0ull ? 63 : __builtin_ctzll(~good) - 1;
+        const int64_t cap_u = last < 0 ? 0 : __shfl(end_u, max(last, 0)), cap_t = last < 0 ? 0 : __shfl(end_t, max(last, 0));
+        if (b < a.B) {
+            a.lay.unit_start[b + 1] = units + (int)(fits ? end_u : cap_u);
+            a.lay.tile_start[b + 1] = tiles + (int)(fits ? end_t : cap_t);
+        }
+        units += (int)cap_u;
+        tiles += (int)cap_t;
+        if (last < 63) a.lay.units = a.lay.tiles = -1;  // nothing behind it
+    }
+}
+// the sequence that place v of the running sums lies in: the last one that starts at v or before it (and is not empty)
+__device__ __forceinline__ int place_of(const int32_t* start, int B, int v) {
+    int lo = 0;
+    for (int step = 1 << (31 - __builtin_clz(B)); step > 0; step >>= 1)
+        if (lo + step <= B && start[lo + step] <= v) lo += step;
+    return lo;
+}
+
+// Decodes units into operands: grid (workgroups, 2), keys and values.  Lane l decodes chain l / 32 of token l % 32.
+constexpr int kExpandWaves = 16;
+constexpr int kTurnStride = 20;  // words per dimension of the tile in which values are turned
+constexpr size_t expand_lds_bytes(int S) { return (table_words(S) + (size_t)kExpandWaves * (kUnitWords + 16 * kTurnStride)) * 4; }
+
+template <bool kLong, bool kValues>
+__device__ __forceinline__ void expand(const TileArgs& a) {
+    extern __shared__ __align__(16) uint32_t smem[];
+    const int S = kValues ? a.Sv : a.Sk;
+    const uint32_t* dev = kValues ? a.dev_v : a.dev_k;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tok = lane & 31, half = lane >> 5;
+    uint32_t* wbuf = smem + table_words(S) + wave * (kUnitWords + 16 * kTurnStride);
+    uint32_t* tile = wbuf + kUnitWords;
+    if (lane < kUnitBlocks) wbuf[lane * kStride + kBlockWords] = 0u;
+    const TableItems items = load_table_items(dev, S);
+    build_tables<kLong>(smem, dev, S, items);
+    const Tables T = table_pointers(smem, S);
+    __syncthreads();
+    const int64_t total = (int64_t)a.lay.unit_start[a.B] * a.Hkv, waves = (int64_t)gridDim.x * kExpandWaves;
+    for (int64_t item = (int64_t)blockIdx.x * kExpandWaves + wave; item < total; item += waves) {
+        const int b = __builtin_amdgcn_readfirstlane(place_of(a.lay.unit_start, a.B, (int)(item / a.Hkv)));
+        const int first = a.lay.unit_start[b], units = a.lay.unit_start[b + 1] - first, at = (int)(item - (int64_t)first * a.Hkv);
+        const int hkv = at / units, u = at - hkv * units, t0 = u * kUnitBlocks;
+        const Sequence seq((args_t*)__builtin_amdgcn_kernarg_segment_ptr(), b);
+        const UnitPages pages = unit_pages(b, t0, seq.kv - 1);
+        bool ok;
+        const UnitLoad pre = load_unit<kValues>(pages, hkv, t0, lane, (tok & 15) | (lane & 32), ok);
+        // (load_unit's lanes 32 on take the unit's second half: here every lane wants the word of token l % 32)
+        const uint32_t other = __shfl(pre.meta, (tok & 15) + 32 * (tok >> 4));
+        const bool there = __shfl((int)ok, 32 * (tok >> 4)) != 0 && t0 + tok < seq.kv;
+        const uint32_t mw = there ? other : 0u;
+        if (!kValues && hkv == 0) {
+            const uint64_t m = __ballot(there);
+            if (lane == 0) a.lay.seen[first + u] = (uint32_t)m;
+        }
+        store_unit(wbuf, pre, lane);
+        const Lane L = lane_setup(T, mw, S);
+        const _Float16 sh16 = __builtin_bit_cast(_Float16, (unsigned short)(mw & 0xFFFFu));
+        const half2_t s2 = {sh16, sh16};
+        uint4* out = a.lay.operands + item * (kUnitBytes / 16) + (kValues ? kUnitBytes / 32 : 0);
+        uint32_t pk[4];
+        const uint32_t swap_sel = (lane & 1) ? 0x03020706u : 0x05040100u;
+        const int pair = tok >> 1, word = (pair & 8) | ((pair >> 1) & 1) << 2 | ((pair >> 2) & 1) << 1 | (pair & 1);  // tokens in the operand's order
+        decode_chain<kLong, kHalf>(wbuf + tok * kStride, half ? L.second_start : 0u, L, [&](int i, uint32_t e) {
+            if ((i & 1) == 0) {
+                pk[(i >> 1) & 3] = e >> 16;
+                return;
+            }
+            pk[(i >> 1) & 3] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, pk[(i >> 1) & 3] | (e & 0xFFFF0000u)) * s2);
+            if ((i & 7) != 7) return;
+            const int j = i >> 3;  // dimensions 64 half + 8 j .. + 7
+            if (!kValues) {
+                out[(half * 4 + (j >> 1)) * 64 + (j & 1) * 32 + tok] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+            } else {
+                wave_lds_fence();
+#pragma unroll
+                for (int r2 = 0; r2 < 4; ++r2) {
+                    const uint32_t mate = (uint32_t)__builtin_amdgcn_mov_dpp((int)pk[r2], 0xB1, 0xF, 0xF, true);  // quad_perm [1,0,3,2]
+                    tile[(8 * half + 2 * r2 + (lane & 1)) * kTurnStride + word] = __builtin_amdgcn_perm(mate, pk[r2], swap_sel);
+                }
+                wave_lds_fence();
+                const int r = lane & 15, part = lane >> 4;  // dimension 64 (r / 8) + 8 j + r % 8, tokens of step part / 2 and lane half part % 2
+                const uint4 v = *reinterpret_cast<const uint4*>(tile + r * kTurnStride + 4 * part);
+                const int d = 64 * (r >> 3) + 8 * j + (r & 7);
+                out[((d >> 5) * 2 + (part >> 1)) * 64 + (part & 1) * 32 + (d & 31)] = v;
+            }
+        });
+    }
+}
+template <bool kLongK, bool kLongV>
+__global__ __launch_bounds__(kExpandWaves * 64) void attend_expand_kernel(TileArgs a) {
+    if (blockIdx.y == 0) expand<kLongK, false>(a);
+    else expand<kLongV, true>(a);
+}
+
+// The products: a workgroup takes a tile of rows of one sequence and key/value head, a wavefront 32 kCols of them, over a range of the sequence's tokens.
+typedef float float16_t __attribute__((ext_vector_type(16)));
+constexpr float kScoreToExp2 = 0.08838834764831845f * 1.4426950408889634f;  // log2(e) / sqrt(128)
+
+template <int kWaves, int kCols, bool kRest>
+__global__ __launch_bounds__(kWaves * 64) void attend_tiles_kernel(TileArgs a) {
+    constexpr int kPieces = kUnitBytes / 16 / (kWaves * 64);  // of a unit per thread, half of them K
+    __shared__ __align__(16) u32x4 lds[2][kUnitBytes / 16];   // two units: K operands, then V operands
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+    const int grp = a.Hq / a.Hkv, hkv = blockIdx.x % a.Hkv, split = blockIdx.y;
+    const int tiles = a.lay.tile_start[a.B], at = tiles - 1 - (int)(blockIdx.x / a.Hkv);  // the last tiles have the most tokens: first
+    if (at < 0) return;
+    const int b = __builtin_amdgcn_readfirstlane(place_of(a.lay.tile_start, a.B, at));
+    const Sequence seq((args_t*)__builtin_amdgcn_kernarg_segment_ptr(), b);
+    const int row_begin = (at - a.lay.tile_start[b]) * a.tile_rows, rows = min(a.tile_rows, seq.n_new * grp - row_begin);
+    const int unit0 = a.lay.unit_start[b], units_b = a.lay.unit_start[b + 1] - unit0;
+    const int T = max(0, seq.kv - seq.n_new + (row_begin + rows - 1) / grp + 1);  // what the last row sees
+    const int units = T > 0 ? units_of(T) : 0, per = (units + a.splits - 1) / a.splits;
+    const int u_begin = min(units, split * per), u_end = min(units, u_begin + per);
+    const u32x4* src = reinterpret_cast<const u32x4*>(a.lay.operands) + ((int64_t)unit0 * a.Hkv + (int64_t)hkv * units_b) * (kUnitBytes / 16);
+    const uint32_t* seen = a.lay.seen + unit0;
+
+    half8_t q[kCols][8];
+    int sees[kCols];
+    size_t out_at[kCols];
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+        const int r = row_begin + min((wave * kCols + c) * 32 + n, rows - 1), token = r / grp, head = hkv * grp + r - token * grp;
+        sees[c] = seq.kv - seq.n_new + token + 1;
+        out_at[c] = ((size_t)(seq.row0 + token) * a.Hq + head) * kGroup;
+        const uint4* from = reinterpret_cast<const uint4*>(a.q + (int64_t)(seq.row0 + token) * a.q_stride + head * kGroup) + h;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) q[c][s] = __builtin_bit_cast(half8_t, from[2 * s]);
+    }
+    float16_t o[kCols][4];
+    float most[kCols], den[kCols];
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+#pragma unroll
+        for (int d = 0; d < 4; ++d) o[c][d] = float16_t{};
+        most[c] = -INFINITY;
+        den[c] = 0.0f;
+    }
+    u32x4 piece[kPieces];
+    const auto load = [&](int u) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) piece[i] = src[(int64_t)min(u, units - 1) * (kUnitBytes / 16) + i * (kWaves * 64) + tid];
+    };
+    const auto keep = [&](int u) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) lds[u & 1][i * (kWaves * 64) + tid] = piece[i];
+    };
+    if (u_begin < u_end) {
+        load(u_begin);
+        keep(u_begin);
+        load(u_begin + 1);
+    }
+    for (int u = u_begin; u < u_end; ++u) {
+        __syncthreads();
+        keep(u + 1);
+        load(u + 2);
+        const half8_t* kop = reinterpret_cast<const half8_t*>(lds[u & 1]) + lane;
+        const half8_t* vop = kop + kUnitBytes / 32;
+        float16_t s[kCols];
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) s[c] = float16_t{};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const half8_t op = kop[k * 64];
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) s[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, q[c][k], s[c], 0, 0, 0);
+        }
+        const uint32_t there = seen[u];
+        half8_t p[kCols][2], rest[kCols][2];
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+            const int left = sees[c] - u * kUnitBlocks;  // tokens of the unit that the row sees
+            if (__ballot(left < kUnitBlocks || there != ~0u) != 0ull) {
+                const uint32_t bits = (left >= 32 ? there : left <= 0 ? 0u : there & ((1u << left) - 1u)) >> (4 * h);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[c][i] = (bits >> (8 * (i / 4) + i % 4)) & 1u ? s[c][i] : -INFINITY;
+            }
+            float mx = s[c][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[c][i]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            const float before = most[c], now = fmaxf(before, mx);
+            if (__ballot(now > before) != 0ull) {
+                const float alpha = before == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((before - now) * kScoreToExp2);
+                most[c] = now;
+                den[c] *= alpha;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) o[c][d] *= alpha;
+            }
+            const float base = now == -INFINITY ? 0.0f : now * kScoreToExp2;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(s[c][i], kScoreToExp2, -base));
+                den[c] += e;
+                const _Float16 e16 = (_Float16)e;
+                p[c][i / 8][i % 8] = e16;
+                if (kRest) rest[c][i / 8][i % 8] = (_Float16)(e - (float)e16);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const half8_t op = vop[(2 * d + k) * 64];
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) {
+                    o[c][d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, p[c][k], o[c][d], 0, 0, 0);
+                    if (kRest) o[c][d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, rest[c][k], o[c][d], 0, 0, 0);
+                }
+            }
+    }
+    // the lane holds dimensions 32 d + 8 (i / 4) + 4 h + i % 4 of its row
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+        den[c] += __shfl_xor(den[c], 32);
+        const int r = (wave * kCols + c) * 32 + n;
+        if (r >= rows) continue;
+        if (a.splits > 1) {
+            const size_t part = ((size_t)at * a.Hkv + hkv) * a.tile_rows * a.splits + (size_t)r * a.splits + split;
+            const size_t all = (size_t)tiles * a.Hkv * a.tile_rows * a.splits;
+            float* to = a.lay.partial + part * kGroup + 4 * h;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *reinterpret_cast<float4_t*>(to + 32 * d + 8 * i) = float4_t{o[c][d][4 * i], o[c][d][4 * i + 1], o[c][d][4 * i + 2], o[c][d][4 * i + 3]};
+            if (h == 0) {
+                a.lay.partial[all * kGroup + part * 2] = most[c] * 0.08838834764831845f;
+                a.lay.partial[all * kGroup + part * 2 + 1] = den[c];
+            }
+            continue;
+        }
+        const float one = den[c] > 0.0f ? 1.0f / den[c] : 0.0f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4_t v = float4_t{o[c][d][4 * i], o[c][d][4 * i + 1], o[c][d][4 * i + 2], o[c][d][4 * i + 3]} * one;
+                const size_t to = out_at[c] + 32 * d + 8 * i + 4 * h;
+                if (a.half) {
+                    typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
+                    *reinterpret_cast<half4_t*>(static_cast<_Float16*>(a.out) + to) = half4_t{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
+                } else {
+                    *reinterpret_cast<float4_t*>(static_cast<float*>(a.out) + to) = v;
+                }
+            }
+    }
+}
+
+// merges the token ranges of a row: grid (tiles that there may be * Hkv, rows of a tile), 128 threads
+__global__ __launch_bounds__(kGroup) void attend_tiles_merge_kernel(TileArgs a) {
+    const int tiles = a.lay.tile_start[a.B], at = blockIdx.x / a.Hkv, hkv = blockIdx.x - at * a.Hkv, grp = a.Hq / a.Hkv;
+    if (at >= tiles) return;
+    const int b = place_of(a.lay.tile_start, a.B, at);
+    const Sequence seq((args_t*)__builtin_amdgcn_kernarg_segment_ptr(), b);
+    const int r = (at - a.lay.tile_start[b]) * a.tile_rows + blockIdx.y, token = r / grp;
+    if (r >= seq.n_new * grp) return;
+    const size_t part = ((size_t)at * a.Hkv + hkv) * a.tile_rows * a.splits + (size_t)blockIdx.y * a.splits, all = (size_t)tiles * a.Hkv * a.tile_rows * a.splits;
+    const float v = merge_splits(a.lay.partial + all * kGroup + part * 2, a.lay.partial + part * kGroup + threadIdx.x, a.splits);
+    store_out((args_t*)__builtin_amdgcn_kernarg_segment_ptr(), ((size_t)(seq.row0 + token) * a.Hq + hkv * grp + r - token * grp) * kGroup + threadIdx.x, v);
+}
+
 // ---- host side -----------------------------------------------------------------------------------------------------------
 struct Plan {
-    int tiles, splits;  // of 16 rows; of the tokens
-    size_t bytes;       // of the workspace
+    int few, tiles, splits;                      // rows taken 16 at a time: up to how many of a sequence; tiles of 16; ranges of the tokens
+    int wide_tiles, tile_rows, wide_splits, units;  // the others: tiles that there may be, their rows, ranges of the tokens, units in the workspace
+    size_t few_bytes, bytes;                     // of the workspace
 };
-Plan plan_of(int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int cus) {
-    Plan p;
-    const long long rows = (long long)std::min(max_new, n_tokens) * (Hq / Hkv);
-    p.tiles = (int)((rows + kGqaMaxGroup - 1) / kGqaMaxGroup);
-    const long long wgs = (long long)B * Hkv * p.tiles;
-    p.splits = (int)std::min<long long>(std::min<long long>(std::max<long long>(1, cus / wgs), ((long long)max_kv + 255) / 256), 256);
-    p.bytes = p.splits > 1 ? (size_t)wgs * kGqaMaxGroup * p.splits * (kGroup + 2) * sizeof(float) : 0;
+constexpr size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
+Plan plan_of(int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv, int cus) {
+    Plan p{};
+    max_new = std::min(max_new, n_tokens);
+    const int grp = Hq / Hkv;
+    const long long rows = (long long)max_new * grp;
+    const bool all = rows > kFewRows && (long long)max_new * B == n_tokens;  // every sequence has as many rows
+    p.few = all ? 0 : kFewRows;
+    if (!all) {
+        p.tiles = (int)((std::min<long long>(rows, kFewRows) + kGqaMaxGroup - 1) / kGqaMaxGroup);
+        const long long wgs = (long long)B * Hkv * p.tiles;
+        p.splits = (int)std::min<long long>(std::min<long long>(std::max<long long>(1, cus / wgs), ((long long)max_kv + 255) / 256), 256);
+        p.few_bytes = p.splits > 1 ? round_up((size_t)wgs * kGqaMaxGroup * p.splits * (kGroup + 2) * sizeof(float)) : 0;
+    }
+    p.bytes = p.few_bytes;
+    if (rows > kFewRows) {
+        p.tile_rows = 128;
+        const long long many = std::min<long long>(B, (long long)n_tokens * grp / ((long long)p.few + 1));  // sequences with more rows than `few`
+        p.wide_tiles = (int)((long long)n_tokens * grp / p.tile_rows + many);
+        const long long units = std::min<long long>((std::min<long long>(total_kv, (long long)many * max_kv)) / kUnitBlocks + many, 0x7FFFFFFF);
+        p.units = (int)units;
+        const long long wgs = (long long)p.wide_tiles * Hkv;
+        p.wide_splits = (int)std::min<long long>(std::min<long long>(std::max<long long>(1, 2 * cus / wgs), ((long long)max_kv + 511) / 512), 64);
+        p.bytes += 2 * round_up(((size_t)B + 1) * 4) + round_up((size_t)units * 4) + (size_t)units * Hkv * kUnitBytes;
+        if (p.wide_splits > 1) p.bytes += round_up((size_t)wgs * p.tile_rows * p.wide_splits * (kGroup + 2) * sizeof(float));
+    }
     return p;
 }
 bool sizes_fit(int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv) {
@@ -440,7 +777,7 @@ extern "C" {
 
 size_t ecco_kv_attend_paged_workspace(int device, int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv) {
     if (n_tokens == 0 || !sizes_fit(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv)) return 0;
-    return plan_of(n_tokens, B, Hq, Hkv, max_new, max_kv, cu_count(device)).bytes;
+    return plan_of(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv, cu_count(device)).bytes;
 }
 
 int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint16_t* q, int64_t q_stride,
@@ -460,17 +797,60 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
     if (model_ready(mk) != ECCO_OK || model_ready(mv) != ECCO_OK || mk->device != mv->device) return ECCO_EINVAL;
     if (n_tokens == 0) return ECCO_OK;
     const int dev_id = mk->device, cus = cu_count(dev_id), shift = __builtin_ctz((unsigned)page_tokens);
-    max_kv = std::min(max_kv, max_pages << shift);
-    const Plan plan = plan_of(n_tokens, B, Hq, Hkv, max_new, max_kv, cus);
+    const Plan plan = plan_of(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv, cus);
     if (plan.bytes > 0 && (!workspace || workspace_bytes < plan.bytes)) return ECCO_EINVAL;
     const bool lk = mk->max_len > kPeekBits, lv = mv->max_len > kPeekBits;
-    const int rows = std::min(kGqaMaxGroup, std::min(max_new, n_tokens) * (Hq / Hkv));
+    max_kv = std::min(max_kv, max_pages << shift);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    PagedArgs args{mk->dev, mv->dev, q, static_cast<const uint4*>(k_blocks), k_meta, static_cast<const uint4*>(v_blocks), v_meta, page_table, q_start, kv_len,
+                   out, static_cast<float*>(workspace), q_stride, mk->S, mv->S, B, Hq, Hkv, n_tokens, n_pages, shift, max_pages, max_kv,
+                   plan.tiles, 0, 0, 0, 0, out_half, plan.few};
+    if (plan.wide_tiles > 0) {
+        char* at = static_cast<char*>(workspace) + plan.few_bytes;
+        const auto part = [&](size_t bytes) {
+            char* p = at;
+            at += round_up(bytes);
+            return p;
+        };
+        TileArgs t{args, {}, plan.tile_rows, plan.wide_splits};
+        t.lay.unit_start = reinterpret_cast<int32_t*>(part(((size_t)B + 1) * 4));
+        t.lay.tile_start = reinterpret_cast<int32_t*>(part(((size_t)B + 1) * 4));
+        t.lay.seen = reinterpret_cast<uint32_t*>(part((size_t)plan.units * 4));
+        t.lay.operands = reinterpret_cast<uint4*>(part((size_t)plan.units * Hkv * kUnitBytes));
+        t.lay.partial = reinterpret_cast<float*>(at);
+        t.lay.units = plan.units;
+        t.lay.tiles = plan.wide_tiles;
+        hipLaunchKernelGGL(attend_layout_kernel, dim3(1), dim3(64), 0, st, t);
+        ECCO_HIP_CHECK(hipGetLastError());
+        const auto expand = [&](auto kernel) -> int {
+            const size_t lds = expand_lds_bytes(std::max(mk->S, mv->S));
+            const int rc = allow_lds(kernel, dev_id, lds);
+            if (rc != ECCO_OK) return rc;
+            const long long wgs = ((long long)plan.units * Hkv + kExpandWaves - 1) / kExpandWaves;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<long long>(wgs, cus / 2), 2), dim3(kExpandWaves * 64), lds, st, t);
+            ECCO_HIP_CHECK(hipGetLastError());
+            return ECCO_OK;
+        };
+        int rc = lk ? (lv ? expand(attend_expand_kernel<true, true>) : expand(attend_expand_kernel<true, false>))
+                    : (lv ? expand(attend_expand_kernel<false, true>) : expand(attend_expand_kernel<false, false>));
+        if (rc != ECCO_OK) return rc;
+        const dim3 grid((unsigned)plan.wide_tiles * Hkv, plan.wide_splits);
+        if (out_half) hipLaunchKernelGGL((attend_tiles_kernel<4, 1, false>), grid, dim3(256), 0, st, t);
+        else hipLaunchKernelGGL((attend_tiles_kernel<4, 1, true>), grid, dim3(256), 0, st, t);
+        ECCO_HIP_CHECK(hipGetLastError());
+        if (plan.wide_splits > 1) {
+            hipLaunchKernelGGL(attend_tiles_merge_kernel, dim3((unsigned)plan.wide_tiles * Hkv, plan.tile_rows), dim3(kGroup), 0, st, t);
+            ECCO_HIP_CHECK(hipGetLastError());
+        }
+    }
+    if (plan.tiles == 0) return ECCO_OK;
+    const int rows = (int)std::min<long long>(kGqaMaxGroup, (long long)std::min(max_new, n_tokens) * (Hq / Hkv));
     const int units = (units_of(max_kv) + plan.splits - 1) / plan.splits;
     const GqaPlan g = gqa_plan(mk->S, lk, mv->S, lv, rows, (size_t)B * Hkv * plan.tiles * plan.splits, units, cus);
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    const PagedArgs args{mk->dev, mv->dev, q, static_cast<const uint4*>(k_blocks), k_meta, static_cast<const uint4*>(v_blocks), v_meta, page_table, q_start, kv_len,
-                         out, static_cast<float*>(workspace), q_stride, mk->S, mv->S, B, Hq, Hkv, n_tokens, n_pages, shift, max_pages, max_kv,
-                         plan.tiles, g.table_words, g.both, g.span, g.step, out_half};
+    args.table_words = g.table_words;
+    args.both = g.both;
+    args.span = g.span;
+    args.step = g.step;
     const auto launch = [&](auto kernel) -> int {
         const int rc = allow_lds(kernel, dev_id, g.lds);
         if (rc != ECCO_OK) return rc;
