@@ -15,6 +15,8 @@ using namespace ecco_chain;
 
 namespace {
 
+typedef float float16_t __attribute__((ext_vector_type(16)));
+
 struct PagedArgs {
     const uint32_t* dev_k;
     const uint32_t* dev_v;
@@ -30,7 +32,7 @@ struct PagedArgs {
     float* ws;
     int64_t q_stride;
     int Sk, Sv, B, Hq, Hkv, n_tokens, n_pages, shift, max_pages, max_kv;
-    int tiles, table_words, both, span, step, half;
+    int table_words, both, span, step, half;
     int few;  // rows of a sequence and key/value head up to which it is taken 16 at a time
 };
 
@@ -81,8 +83,7 @@ __device__ __forceinline__ UnitPages unit_pages(int b, int t0, int last) {
     p.page[1] = row[(min(t0 + kUnitBlocks / 2, last) >> a->shift) + zero];
     return p;
 }
-// As load_unit of the contiguous caches: the payload pieces of this lane and the meta word of the unit's block `tok`, which it decodes (tokens
-// 16 on belong to lanes 32 on).  Slots of a page are all readable, whether they hold a token or not; of a page that is none the first one's are read.
+// As load_unit of the contiguous caches: the payload pieces of this lane and the meta word of the unit's block `tok`, which it decodes.  Slots of a page are all readable, whether they hold a token or not; of a page that is none the first one's are read.
 // ok: whether the page of token `tok` is one
 template <bool kValues>
 __device__ __forceinline__ UnitLoad load_unit(const UnitPages& p, int hkv, int t0, int lane, int tok, bool& ok) {
@@ -98,35 +99,41 @@ __device__ __forceinline__ UnitLoad load_unit(const UnitPages& p, int hkv, int t
     UnitLoad u;
     u.v0 = make_uint4(v0.x, v0.y, v0.z, v0.w);
     u.v1 = make_uint4(v1.x, v1.y, v1.z, v1.w);
-    u.meta = meta[(lane < 32 ? at[0] : at[1]) + (tok & 15)];
-    ok = in_pool(lane < 32 ? p.page[0] : p.page[1], a->n_pages);
+    u.meta = meta[(tok < 16 ? at[0] : at[1]) + (tok & 15)];
+    ok = in_pool(tok < 16 ? p.page[0] : p.page[1], a->n_pages);
     return u;
 }
 
 // ---- few rows per key/value head ---------------------------------------------------------------------------------------
 // The rows of a sequence and a key/value head are its new tokens times the grp = Hq / Hkv query heads that share it, row r being head r % grp of
-// new token r / grp.  A workgroup takes up to 16 of them over a range of the sequence's tokens, and decodes every K and V block of the range on
-// the way into the products, as the grouped-query kernel over contiguous caches does (kv_attend_gqa_kernel says how tiles, halves and rests lie; the
-// columns here are rows in this sense, each with an end of its own: what a token sees ends with itself).
-// grid: (B * Hkv, n_splits, tiles of 16 rows).  The partial result of a split and row is at index ((sequence and head * tiles + tile) * 16
-// + row) * n_splits + split of the workspace: 128 outputs each, then (maximum, denominator) pairs.
-template <bool kLongK, bool kLongV, bool kWide, int kWaves>
-__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWaves == 12 ? 3 : 4))) void attend_rows_kernel(PagedArgs) {
+// new token r / grp.  A workgroup takes up to kRows of them (8, 16 or 32) over a range of the sequence's tokens, and decodes every K and V block of
+// the range on the way into the products, as the grouped-query kernel over contiguous caches does (kv_attend_gqa_kernel says how tiles, halves
+// and rests lie; the columns here are rows in this sense, each with an end of its own: what a token sees ends with itself).  From 9 rows on the
+// scores come from v_mfma_f32_32x32x16_f16 instead: one product per eight values and chain for 32 tokens and up to 32 rows, no half of its operand
+// zeroed, eight query values of one row per lane (lane l decodes chain l / 32 of token l % 32).  With 32 rows the second product runs over two tiles
+// of 16.
+// grid: (B * Hkv, n_splits).  The partial result of a split and row is at index ((sequence and head) * kRows + row) * n_splits + split of the
+// workspace: 128 outputs each, then (maximum, denominator) pairs.
+template <bool kLongK, bool kLongV, int kRows, int kWaves>
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWaves == 12 ? 3 : kRows > 8 ? 2 : 4))) void attend_rows_kernel(PagedArgs) {
     constexpr int kThreads = kWaves * 64;
     static_assert(2 * kThreads >= kMaxS * kK, "load_table_items: two table items per thread cover every model");
-    constexpr int kOutputs = (kGqaMaxGroup * kGroup + kThreads - 1) / kThreads;  // output elements per thread
+    constexpr bool kWide = kRows > 8;
+    constexpr int kTiles = kRows == 32 ? 2 : 1, kTileRows = kRows / kTiles;  // of the second product
+    constexpr int kOutputs = (kTileRows * kGroup + kThreads - 1) / kThreads;  // output elements per thread and tile
+    // (one more register than the allocation that bodies of up to 16 rows end in: none of its 64-bit shifts may have its amount in the last one, see build.py)
+    if constexpr (kWide) asm volatile("" ::: "v136");
     args_t* const first = fresh_args();
     const int both = first->both, table_words = first->table_words, Hkv = first->Hkv;
     extern __shared__ __align__(16) uint32_t smem[];
     const int grp = first->Hq / Hkv, sstride = gqa_score_stride(first->span);
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int b = blockIdx.x / Hkv, hkv = blockIdx.x - b * Hkv, split = blockIdx.y, row_begin = blockIdx.z * kGqaMaxGroup;
+    const int b = blockIdx.x / Hkv, hkv = blockIdx.x - b * Hkv, split = blockIdx.y;
     const Sequence seq(first, b);
-    const int rows = min(kGqaMaxGroup, seq.n_new * grp - row_begin);
-    if (rows <= 0 || seq.n_new * grp > first->few) return;  // uniform, ahead of every barrier
-    float* state = reinterpret_cast<float*>(smem);  // [wavefront][16] maxima, [wavefront][16] denominators
-    uint32_t* k_tables = smem + gqa_state_words(kWaves);
+    const int rows = seq.n_new * grp;
+    if (rows <= 0 || rows > first->few) return;  // uniform, ahead of every barrier
+    uint32_t* k_tables = smem;
     uint32_t* wbuf = k_tables + table_words + wave * kUnitWords;
     uint32_t* tile = k_tables + table_words + kWaves * kUnitWords + wave * kTileWords;
     float* scores = reinterpret_cast<float*>(k_tables + table_words + kWaves * (kUnitWords + kTileWords));  // [rows][sstride]
@@ -134,7 +141,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
     if (lane < kUnitBlocks) wbuf[lane * kStride + kBlockWords] = 0u;
 
     // the last row's token sees the most: T tokens
-    const int T = max(0, seq.kv - seq.n_new + (row_begin + rows - 1) / grp + 1), last = T - 1;
+    const int T = max(0, seq.kv), last = T - 1;
     const int n_splits = gridDim.y;
     const int64_t per_range = (int64_t)((units_of(max(T, 1)) + n_splits - 1) / n_splits) * kUnitBlocks;
     const int t_begin = (int)min((int64_t)T, split * per_range), t_end = (int)min((int64_t)T, (split + 1) * per_range);
@@ -144,10 +151,15 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
         __device__ Place() : lane(fresh_thread() & 63), n(lane & 15), slice(lane >> 4), half(slice & 1), tok(n + 16 * (lane >> 5)) {}
     };
     const float inv_sqrt_d = 0.08838834764831845f;  // 1 / sqrt(128)
-    float4_t o[8];  // tile j: row r is dimension 64 (r / 8) + 8 j + r % 8, column the row
+    float4_t o[kTiles][8];  // tile j: row r is dimension 64 (r / 8) + 8 j + r % 8, column the row
+    float run_max[kTiles], run_den[kTiles];  // of this wavefront and of row l % 16 of the tile; the denominator of the lane's tokens
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    float run_max = -INFINITY, run_den = 0.0f;  // of this wavefront and of row l % 16; the denominator of the lane's tokens
+    for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[t][j] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        run_max[t] = -INFINITY;
+        run_den[t] = 0.0f;
+    }
 
     for (int s0 = t_begin; s0 < t_end; s0 += span_max) {
         const int span = min(span_max, t_end - s0);
@@ -160,11 +172,10 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
         float mx = -INFINITY;
         {
         const Place P;
-        const int lane = P.lane, n = P.n, slice = P.slice, half = P.half, tok = P.tok;
+        const int lane = P.lane, n = kWide ? lane & 31 : P.n, slice = P.slice, half = kWide ? lane >> 5 : P.half, tok = kWide ? n : P.tok;
         const int row = kWide ? n : n & 7;                              // row of this lane's column
         const bool row_ok = row < rows, b_ok = row_ok && (kWide || (n >> 3) == (lane >> 5));
-        const int r = row_begin + min(row, rows - 1), token = r / grp;
-        
+        const int r = min(row, rows - 1), token = r / grp;
         const int sees = min(span, seq.kv - seq.n_new + token + 1 - s0);  // tokens of the span
         int u = wave;
         const auto load_k = [&](int at) { pre = load_unit<false>(now, hkv, s0 + min(at, units - 1) * kUnitBlocks, lane, tok, pre_ok); };
@@ -208,10 +219,11 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
         for (int j = 0; j < kHalf / 8; ++j) bq[j] = b_ok ? bq[j] : make_uint4(0u, 0u, 0u, 0u);
         for (; u < units; u += kWaves) {
             store_unit(wbuf, pre, lane);
-            // a slot past the range, or of no page, may hold anything: scale 0, so that its values are zeros (tokens m and 16 + m share a row
-            // of the product, and NaN * 0 would poison it)
+            // a slot past the range, or of no page, may hold anything: scale 0, so that its values are zeros (up to 8 rows, tokens m and 16 + m share
+            // a row of the product, and NaN * 0 would poison it)
             const uint32_t mw = u * kUnitBlocks + tok < span && pre_ok ? pre.meta : (pre.meta & 0xFFFF0000u);
-            const uint64_t pool = __ballot(pre_ok);  // bits 0 and 32: of the unit's two halves
+            const uint64_t pool = __ballot(pre_ok);
+            const bool ok0 = (pool & 1u) != 0u, ok1 = ((pool >> (kWide ? 16 : 32)) & 1u) != 0u;  // of the unit's two halves
             if (u + kWaves < units) {
                 now = next;
                 load_k(u + kWaves);
@@ -221,7 +233,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
             const _Float16 sh16 = __builtin_bit_cast(_Float16, (unsigned short)(mw & 0xFFFFu));
             const half2_t s2 = {sh16, sh16};
             uint32_t pk[4];
-            float4_t acc[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+            std::conditional_t<kWide, float16_t, float4_t> acc = {};
             decode_chain<kLongK, kHalf>(wbuf + tok * kStride, half ? L.second_start : 0u, L, [&](int i, uint32_t e) {
                 if ((i & 1) == 0) {
                     pk[(i >> 1) & 3] = e >> 16;
@@ -230,34 +242,30 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
                 pk[(i >> 1) & 3] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, pk[(i >> 1) & 3] | (e & 0xFFFF0000u)) * s2);
                 if ((i & 7) != 7) return;
                 const half8_t bv = __builtin_bit_cast(half8_t, bq[i >> 3]);
-                if (kWide) {
-                    const bool low = lane < 32;
-                    const uint4 a0 = make_uint4(low ? pk[0] : 0u, low ? pk[1] : 0u, low ? pk[2] : 0u, low ? pk[3] : 0u);
-                    const uint4 a1 = make_uint4(low ? 0u : pk[0], low ? 0u : pk[1], low ? 0u : pk[2], low ? 0u : pk[3]);
-                    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a0), bv, acc[0], 0, 0, 0);
-                    acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a1), bv, acc[1], 0, 0, 0);
-                } else {
-                    const uint4 av = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-                    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, av), bv, acc[0], 0, 0, 0);
-                }
+                const half8_t av = __builtin_bit_cast(half8_t, make_uint4(pk[0], pk[1], pk[2], pk[3]));
+                if constexpr (kWide) acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(av, bv, acc, 0, 0, 0);
+                else acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(av, bv, acc, 0, 0, 0);
             });
-            // accumulator layout of the 16 x 16 tile: register i of lane l is row 4 * (l / 16) + i, column l % 16
+            // accumulator layouts: register i of lane l of a 16 x 16 tile is row 4 * (l / 16) + i, column l % 16; of a 32 x 32 one row
+            // 8 (i / 4) + 4 (l / 32) + i % 4, column l % 32
 #pragma unroll
-            for (int w = 0; w < (kWide ? 2 : 1); ++w) {
-                const bool upper = kWide ? w != 0 : n >= 8, ok = (upper ? (uint32_t)(pool >> 32) : (uint32_t)pool) != 0u;  // of the unit's tokens
-                const int t0 = u * kUnitBlocks + 4 * slice + (upper ? 16 : 0);
+            for (int w = 0; w < (kWide ? 4 : 1); ++w) {
+                const bool upper = kWide ? w >= 2 : n >= 8, ok = upper ? ok1 : ok0;  // of the unit's tokens
+                const int t0 = u * kUnitBlocks + (kWide ? 8 * w + 4 * half : 4 * slice + (upper ? 16 : 0));
                 float4_t v;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    v[i] = ok && t0 + i < sees ? acc[w][i] * inv_sqrt_d : -INFINITY;
+                    v[i] = ok && t0 + i < sees ? acc[4 * w + i] * inv_sqrt_d : -INFINITY;
                     mx = fmaxf(mx, v[i]);
                 }
                 if (row_ok) *reinterpret_cast<float4_t*>(scores + row * sstride + t0) = v;  // for this wavefront alone
             }
         }
         // the wavefront's maximum per row: over the lanes of the column
-        if (!kWide) mx = fmaxf(mx, __shfl_xor(mx, 8));
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        if (!kWide) {
+            mx = fmaxf(mx, __shfl_xor(mx, 8));
+            mx = fmaxf(mx, __shfl_xor(mx, 16));
+        }
         mx = fmaxf(mx, __shfl_xor(mx, 32));
         }
         // ---- weighted sum of V over the span
@@ -281,17 +289,20 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
         }
         const int Sv = fresh_args()->Sv;
         const Tables TV = table_pointers(v_tables, Sv);
-        const float before = run_max;
-        run_max = fmaxf(before, mx);
-        const float base = run_max == -INFINITY ? 0.0f : run_max;  // (a wavefront without units, or without a score above -inf)
-        if (s0 != t_begin) {  // every accumulator of a lane belongs to row l % 16
-            const float alpha = before == -INFINITY ? 0.0f : __expf(before - base);
-            run_den *= alpha;
+        float base[kTiles];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] *= alpha;
+        for (int t = 0; t < kTiles; ++t) {
+            const float before = run_max[t];
+            run_max[t] = fmaxf(before, kWide ? __shfl(mx, 16 * t + n) : mx);
+            base[t] = run_max[t] == -INFINITY ? 0.0f : run_max[t];  // (a wavefront without units, or without a score above -inf)
+            if (s0 != t_begin) {  // every accumulator of a lane belongs to row l % 16
+                const float alpha = before == -INFINITY ? 0.0f : __expf(before - base[t]);
+                run_den[t] *= alpha;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[t][j] *= alpha;
+            }
         }
         const int row = kWide ? n : n & 7;
-        const float* score = scores + min(row, rows - 1) * sstride + 8 * slice;
         for (; u < units; u += kWaves) {
             store_unit(wbuf, pre, lane);
             const uint32_t mw = u * kUnitBlocks + tok < span && pre_ok ? pre.meta : (pre.meta & 0xFFFF0000u);
@@ -303,20 +314,22 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
             const Lane L = lane_setup(TV, mw, Sv);
             const _Float16 sh16 = __builtin_bit_cast(_Float16, (unsigned short)(mw & 0xFFFFu));
             const half2_t s2 = {sh16, sh16};
-            // B operand: probabilities of row l % 16 for tokens 8 * (l / 16) .. + 7 of the unit, 0 for what is not seen.  What an
+            // B operand: probabilities of row l % 16 of the tile for tokens 8 * (l / 16) .. + 7 of the unit, 0 for what is not seen.  What an
             // FP16 probability leaves of the FP32 one is the operand of a product of its own, or with up to eight rows of columns 8..15.
             const float taken = !kWide && n < 8 ? 0.0f : 1.0f;
-            half8_t pb, rest;
-            {
-                const float4_t s[2] = {reinterpret_cast<const float4_t*>(score + u * kUnitBlocks)[0], reinterpret_cast<const float4_t*>(score + u * kUnitBlocks)[1]};
+            half8_t pb[kTiles], rest[kTiles];
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                const float* score = scores + min(16 * t + row, rows - 1) * sstride + 8 * slice + u * kUnitBlocks;
+                const float4_t s[2] = {reinterpret_cast<const float4_t*>(score)[0], reinterpret_cast<const float4_t*>(score)[1]};
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float p = row < rows ? __expf(s[i >> 2][i & 3] - base) : 0.0f;
-                    pb[i] = (_Float16)p;
-                    rest[i] = (_Float16)fmaf(-taken, (float)pb[i], p);
-                    run_den += p;
+                    const float p = 16 * t + row < rows ? __expf(s[i >> 2][i & 3] - base[t]) : 0.0f;
+                    pb[t][i] = (_Float16)p;
+                    rest[t][i] = (_Float16)fmaf(-taken, (float)pb[t][i], p);
+                    run_den[t] += p;
                 }
-                if (!kWide) pb = rest;
+                if (!kWide) pb[t] = rest[t];
             }
             uint32_t pk[4];
             decode_chain<kLongV, kHalf>(wbuf + tok * kStride, half ? L.second_start : 0u, L, [&](int i, uint32_t e) {
@@ -336,84 +349,92 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
                 }
                 wave_lds_fence();
                 const uint4 a0 = *reinterpret_cast<const uint4*>(tile + n * kTileStride + 4 * slice);
-                o[i >> 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a0), pb, o[i >> 3], 0, 0, 0);
-                if (kWide) o[i >> 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a0), rest, o[i >> 3], 0, 0, 0);
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    o[t][i >> 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a0), pb[t], o[t][i >> 3], 0, 0, 0);
+                    if (kWide) o[t][i >> 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a0), rest[t], o[t][i >> 3], 0, 0, 0);
+                }
             });
         }
     }
-    // ---- sum over the wavefronts; everything in LDS but the state is dead behind the first barrier
+    // ---- sum over the wavefronts, a tile of rows after the other; everything in LDS is dead behind the first barrier
     const Place P;
     const int n = P.n, slice = P.slice;
     args_t* const a = fresh_args();
     float* const ws = a->ws;
-    const int n_tiles = a->tiles;
-    const size_t part = ((size_t)blockIdx.x * n_tiles + blockIdx.z) * kGqaMaxGroup * n_splits + split;  // of the tile's first row
-    const size_t total = (size_t)gridDim.x * n_tiles * kGqaMaxGroup * n_splits;
-    run_den += __shfl_xor(run_den, 16);
-    run_den += __shfl_xor(run_den, 32);
-    if (lane < 16) state[wave * kGqaMaxGroup + lane] = run_max;
-    __syncthreads();
-    float most = -INFINITY;
+    const size_t part = (size_t)blockIdx.x * kRows * n_splits + split;  // of the first row
+    const size_t total = (size_t)gridDim.x * kRows * n_splits;
+    float* red = reinterpret_cast<float*>(smem);  // [wavefront][8 tiles][4 slices][16 lanes][4]
+    float* state = red + kWaves * 8 * kRedTile;   // [wavefront][16] maxima, [wavefront][16] denominators
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) most = fmaxf(most, state[w * kGqaMaxGroup + n]);
-    const float mine = run_max == -INFINITY ? 0.0f : __expf(run_max - most);
-    if (lane < 16) state[(kWaves + wave) * kGqaMaxGroup + lane] = run_den * mine;
-    float* red = reinterpret_cast<float*>(k_tables);  // [wavefront][8 tiles][4 slices][16 lanes][4]
-    if (!kWide) {  // what the rests contributed
+    for (int t = 0; t < kTiles; ++t) {
+        run_den[t] += __shfl_xor(run_den[t], 16);
+        run_den[t] += __shfl_xor(run_den[t], 32);
+        __syncthreads();
+        if (lane < 16) state[wave * kGqaMaxGroup + lane] = run_max[t];
+        __syncthreads();
+        float most = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int w = 0; w < kWaves; ++w) most = fmaxf(most, state[w * kGqaMaxGroup + n]);
+        const float mine = run_max[t] == -INFINITY ? 0.0f : __expf(run_max[t] - most);
+        if (lane < 16) state[(kWaves + wave) * kGqaMaxGroup + lane] = run_den[t] * mine;
+        if (!kWide) {  // what the rests contributed
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float here = o[j][i];
-                o[j][i] = here + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, here), 0x128, 0xF, 0xF, true));  // row_ror:8
+            for (int j = 0; j < 8; ++j) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float here = o[t][j][i];
+                    o[t][j][i] = here + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, here), 0x128, 0xF, 0xF, true));  // row_ror:8
+                }
             }
         }
-    }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) *reinterpret_cast<float4_t*>(red + (wave * 8 + j) * kRedTile + slice * kRedRow + n * 4) = o[j] * mine;
-    __syncthreads();
-    const auto denominator = [&](int g) {
-        float den = 0.0f;
+        for (int j = 0; j < 8; ++j) *reinterpret_cast<float4_t*>(red + (wave * 8 + j) * kRedTile + slice * kRedRow + n * 4) = o[t][j] * mine;
+        __syncthreads();
+        const auto denominator = [&](int g) {
+            float den = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) den += state[(kWaves + w) * kGqaMaxGroup + g];
-        return den;
-    };
-    if (n_splits > 1 && tid < rows) {  // (the first wavefront's lane of row `tid` holds that row's maximum)
-        const size_t at = total * kGroup + (part + (size_t)tid * n_splits) * 2;
-        ws[at] = most;
-        ws[at + 1] = denominator(tid);
-    }
+            for (int w = 0; w < kWaves; ++w) den += state[(kWaves + w) * kGqaMaxGroup + g];
+            return den;
+        };
+        const int here = min(rows - 16 * t, kTileRows);  // rows of the tile
+        if (n_splits > 1 && tid < here) {  // (the first wavefront's lane of row `tid` holds that row's maximum)
+            const size_t at = total * kGroup + (part + (size_t)(16 * t + tid) * n_splits) * 2;
+            ws[at] = most;
+            ws[at + 1] = denominator(tid);
+        }
 #pragma unroll
-    for (int k = 0; k < kOutputs; ++k) {
-        const int e = tid + k * kThreads, g = e / kGroup, dim = e % kGroup;
-        if (g < rows) {
-            const int at_row = 8 * (dim >> 6) + (dim & 7);
-            const float* at = red + ((dim & 63) >> 3) * kRedTile + (at_row >> 2) * kRedRow + g * 4 + (at_row & 3);
-            float sum = 0.0f;
+        for (int k = 0; k < kOutputs; ++k) {
+            const int e = tid + k * kThreads, g = e / kGroup, dim = e % kGroup;
+            if (g < here) {
+                const int at_row = 8 * (dim >> 6) + (dim & 7);
+                const float* at = red + ((dim & 63) >> 3) * kRedTile + (at_row >> 2) * kRedRow + g * 4 + (at_row & 3);
+                float sum = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) sum += at[w * 8 * kRedTile];
-            if (n_splits == 1) {
-                const float den = denominator(g);
-                const int r = row_begin + g, token = r / grp;
-                store_out(a, ((size_t)(seq.row0 + token) * a->Hq + hkv * grp + r - token * grp) * kGroup + dim, den > 0.0f ? sum / den : 0.0f);
-            } else {
-                ws[(part + (size_t)g * n_splits) * kGroup + dim] = sum;
+                for (int w = 0; w < kWaves; ++w) sum += at[w * 8 * kRedTile];
+                const int r = 16 * t + g;
+                if (n_splits == 1) {
+                    const float den = denominator(g);
+                    const int token = r / grp;
+                    store_out(a, ((size_t)(seq.row0 + token) * a->Hq + hkv * grp + r - token * grp) * kGroup + dim, den > 0.0f ? sum / den : 0.0f);
+                } else {
+                    ws[(part + (size_t)r * n_splits) * kGroup + dim] = sum;
+                }
             }
         }
     }
 }
 
-// merges the token ranges of a row: grid (B * Hkv, rows of a tile that there may be, tiles), 128 threads
-__global__ __launch_bounds__(kGroup) void attend_rows_merge_kernel(PagedArgs args, int n_splits) {
+// merges the token ranges of a row: grid (B * Hkv, rows that there may be), 128 threads
+__global__ __launch_bounds__(kGroup) void attend_rows_merge_kernel(PagedArgs args, int tile_rows, int n_splits) {
     args_t* const a = fresh_args();
     const int b = blockIdx.x / args.Hkv, hkv = blockIdx.x - b * args.Hkv, grp = args.Hq / args.Hkv;
     const Sequence seq(a, b);
-    const int r = blockIdx.z * kGqaMaxGroup + blockIdx.y, token = r / grp;
+    const int r = blockIdx.y, token = r / grp;
     if (r >= seq.n_new * grp || seq.n_new * grp > args.few) return;
-    const size_t at = (((size_t)blockIdx.x * args.tiles + blockIdx.z) * kGqaMaxGroup + blockIdx.y) * n_splits;
-    const size_t total = (size_t)gridDim.x * args.tiles * kGqaMaxGroup * n_splits;
+    const size_t at = ((size_t)blockIdx.x * tile_rows + r) * n_splits, total = (size_t)gridDim.x * tile_rows * n_splits;
     const float v = merge_splits(args.ws + total * kGroup + at * 2, args.ws + at * kGroup + threadIdx.x, n_splits);
-    store_out(a, ((size_t)(seq.row0 + token) * args.Hq + hkv * grp + r - token * grp) * kGroup + threadIdx.x, v);
+    store_out(a, ((size_t)(seq.row0 + token) * a->Hq + hkv * grp + r - token * grp) * kGroup + threadIdx.x, v);
 }
 
 // ---- many rows per key/value head ----------------------------------------------------------------------------------------
@@ -426,7 +447,6 @@ __global__ __launch_bounds__(kGroup) void attend_rows_merge_kernel(PagedArgs arg
 //       l takes dimension 32 d + l % 32 and the tokens 16 s + 4 (l / 32) + (0 1 2 3 8 9 10 11): those whose scores the lane holds after the
 //       first product, so that probabilities become B operands where they are
 // so a unit is copied to LDS as it is, and read from there without bank conflicts.
-constexpr int kFewRows = 2 * kGqaMaxGroup;
 constexpr int kUnitHalves = kUnitBlocks * kGroup;      // FP16 values of a unit's K, or V
 constexpr int kUnitBytes = 2 * kUnitHalves * 2;
 
@@ -517,11 +537,9 @@ __device__ __forceinline__ void expand(const TileArgs& a) {
         const Sequence seq((args_t*)__builtin_amdgcn_kernarg_segment_ptr(), b);
         const UnitPages pages = unit_pages(b, t0, seq.kv - 1);
         bool ok;
-        const UnitLoad pre = load_unit<kValues>(pages, hkv, t0, lane, (tok & 15) | (lane & 32), ok);
-        // (load_unit's lanes 32 on take the unit's second half: here every lane wants the word of token l % 32)
-        const uint32_t other = __shfl(pre.meta, (tok & 15) + 32 * (tok >> 4));
-        const bool there = __shfl((int)ok, 32 * (tok >> 4)) != 0 && t0 + tok < seq.kv;
-        const uint32_t mw = there ? other : 0u;
+        const UnitLoad pre = load_unit<kValues>(pages, hkv, t0, lane, tok, ok);
+        const bool there = ok && t0 + tok < seq.kv;
+        const uint32_t mw = there ? pre.meta : 0u;
         if (!kValues && hkv == 0) {
             const uint64_t m = __ballot(there);
             if (lane == 0) a.lay.seen[first + u] = (uint32_t)m;
@@ -567,13 +585,20 @@ __global__ __launch_bounds__(kExpandWaves * 64) void attend_expand_kernel(TileAr
 }
 
 // The products: a workgroup takes a tile of rows of one sequence and key/value head, a wavefront 32 kCols of them, over a range of the sequence's tokens.
-typedef float float16_t __attribute__((ext_vector_type(16)));
 constexpr float kScoreToExp2 = 0.08838834764831845f * 1.4426950408889634f;  // log2(e) / sqrt(128)
 
-template <int kWaves, int kCols, bool kRest>
-__global__ __launch_bounds__(kWaves * 64) void attend_tiles_kernel(TileArgs a) {
-    constexpr int kPieces = kUnitBytes / 16 / (kWaves * 64);  // of a unit per thread, half of them K
-    __shared__ __align__(16) u32x4 lds[2][kUnitBytes / 16];   // two units: K operands, then V operands
+// the larger of the two lanes' values that hold a row's scores, l and l + 32
+__device__ __forceinline__ float halves_max(float v) {
+    const uint32_t x = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+
+template <int kWaves, bool kRest>
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void attend_tiles_kernel(TileArgs a) {
+    constexpr int kPair = 2 * kUnitBytes / 16;            // sixteen-byte pieces of two units
+    constexpr int kPieces = kPair / (kWaves * 64);        // per thread
+    __shared__ __align__(16) u32x4 lds[2][kPair];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
     const int grp = a.Hq / a.Hkv, hkv = blockIdx.x % a.Hkv, split = blockIdx.y;
     const int tiles = a.lay.tile_start[a.B], at = tiles - 1 - (int)(blockIdx.x / a.Hkv);  // the last tiles have the most tokens: first
@@ -583,140 +608,138 @@ __global__ __launch_bounds__(kWaves * 64) void attend_tiles_kernel(TileArgs a) {
     const int row_begin = (at - a.lay.tile_start[b]) * a.tile_rows, rows = min(a.tile_rows, seq.n_new * grp - row_begin);
     const int unit0 = a.lay.unit_start[b], units_b = a.lay.unit_start[b + 1] - unit0;
     const int T = max(0, seq.kv - seq.n_new + (row_begin + rows - 1) / grp + 1);  // what the last row sees
-    const int units = T > 0 ? units_of(T) : 0, per = (units + a.splits - 1) / a.splits;
+    const int units = T > 0 ? units_of(T) : 0, per = ((units + 1) / 2 + a.splits - 1) / a.splits * 2;
     const int u_begin = min(units, split * per), u_end = min(units, u_begin + per);
     const u32x4* src = reinterpret_cast<const u32x4*>(a.lay.operands) + ((int64_t)unit0 * a.Hkv + (int64_t)hkv * units_b) * (kUnitBytes / 16);
     const uint32_t* seen = a.lay.seen + unit0;
 
-    half8_t q[kCols][8];
-    int sees[kCols];
-    size_t out_at[kCols];
-#pragma unroll
-    for (int c = 0; c < kCols; ++c) {
-        const int r = row_begin + min((wave * kCols + c) * 32 + n, rows - 1), token = r / grp, head = hkv * grp + r - token * grp;
-        sees[c] = seq.kv - seq.n_new + token + 1;
-        out_at[c] = ((size_t)(seq.row0 + token) * a.Hq + head) * kGroup;
+    const int r = row_begin + min(wave * 32 + n, rows - 1), token = r / grp, head = hkv * grp + r - token * grp;
+    const int sees = min(seq.kv - seq.n_new + token + 1, u_end * kUnitBlocks);
+    const size_t out_at = ((size_t)(seq.row0 + token) * a.Hq + head) * kGroup;
+    half8_t q[8];
+    {
         const uint4* from = reinterpret_cast<const uint4*>(a.q + (int64_t)(seq.row0 + token) * a.q_stride + head * kGroup) + h;
 #pragma unroll
-        for (int s = 0; s < 8; ++s) q[c][s] = __builtin_bit_cast(half8_t, from[2 * s]);
+        for (int s = 0; s < 8; ++s) q[s] = __builtin_bit_cast(half8_t, from[2 * s]);
     }
-    float16_t o[kCols][4];
-    float most[kCols], den[kCols];
+    // units in front of which every row of the wavefront sees every token (rows are in the order of their tokens: the first sees the least)
+    const int whole = __builtin_amdgcn_readfirstlane(max(sees, 0)) / kUnitBlocks;
+    float16_t o[4];
 #pragma unroll
-    for (int c = 0; c < kCols; ++c) {
-#pragma unroll
-        for (int d = 0; d < 4; ++d) o[c][d] = float16_t{};
-        most[c] = -INFINITY;
-        den[c] = 0.0f;
-    }
+    for (int d = 0; d < 4; ++d) o[d] = float16_t{};
+    float most = -INFINITY, den = 0.0f;
     u32x4 piece[kPieces];
+    uint32_t seen0, seen1;
     const auto load = [&](int u) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) piece[i] = src[(int64_t)min(u, units - 1) * (kUnitBytes / 16) + i * (kWaves * 64) + tid];
+        for (int i = 0; i < kPieces; ++i) {
+            const int unit = u + i * (kWaves * 64) / (kPair / 2);
+            piece[i] = src[(int64_t)min(unit, units - 1) * (kUnitBytes / 16) + i * (kWaves * 64) % (kPair / 2) + tid];
+        }
+        seen0 = seen[min(u, units - 1)];
+        seen1 = seen[min(u + 1, units - 1)];
     };
-    const auto keep = [&](int u) {
+    const auto keep = [&](int which) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) lds[u & 1][i * (kWaves * 64) + tid] = piece[i];
+        for (int i = 0; i < kPieces; ++i) lds[which][i * (kWaves * 64) + tid] = piece[i];
     };
+    static_assert(kWaves * 64 <= kPair / 2, "a round of the threads stays inside a unit");
     if (u_begin < u_end) {
         load(u_begin);
-        keep(u_begin);
-        load(u_begin + 1);
+        keep(0);
     }
-    for (int u = u_begin; u < u_end; ++u) {
-        __syncthreads();
-        keep(u + 1);
+    constexpr float kAhead = 8.0f;
+    int which = 0;
+    for (int u = u_begin; u < u_end; u += 2, which ^= 1) {
+        const uint32_t there0 = seen0, there1 = seen1;
         load(u + 2);
-        const half8_t* kop = reinterpret_cast<const half8_t*>(lds[u & 1]) + lane;
-        const half8_t* vop = kop + kUnitBytes / 32;
-        float16_t s[kCols];
+        __syncthreads();
+        const half8_t* op = reinterpret_cast<const half8_t*>(lds[which]) + lane;
+        float16_t s[2];
 #pragma unroll
-        for (int c = 0; c < kCols; ++c) s[c] = float16_t{};
+        for (int k = 0; k < 8; ++k)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const half8_t op = kop[k * 64];
+            for (int w = 0; w < 2; ++w) s[w] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op[w * (kPair / 2) + k * 64], q[k], k == 0 ? float16_t{} : s[w], 0, 0, 0);
+        // six operands ahead of the products
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
 #pragma unroll
-            for (int c = 0; c < kCols; ++c) s[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, q[c][k], s[c], 0, 0, 0);
+        for (int k = 0; k < 10; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
-        const uint32_t there = seen[u];
-        half8_t p[kCols][2], rest[kCols][2];
+        __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
+        if (u + 2 > whole || (__builtin_amdgcn_readfirstlane(there0) & __builtin_amdgcn_readfirstlane(there1)) != ~0u) {
 #pragma unroll
-        for (int c = 0; c < kCols; ++c) {
-            const int left = sees[c] - u * kUnitBlocks;  // tokens of the unit that the row sees
-            if (__ballot(left < kUnitBlocks || there != ~0u) != 0ull) {
+            for (int w = 0; w < 2; ++w) {
+                const int left = sees - (u + w) * kUnitBlocks;
+                const uint32_t there = w ? there1 : there0;
                 const uint32_t bits = (left >= 32 ? there : left <= 0 ? 0u : there & ((1u << left) - 1u)) >> (4 * h);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[c][i] = (bits >> (8 * (i / 4) + i % 4)) & 1u ? s[c][i] : -INFINITY;
-            }
-            float mx = s[c][0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[c][i]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            const float before = most[c], now = fmaxf(before, mx);
-            if (__ballot(now > before) != 0ull) {
-                const float alpha = before == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((before - now) * kScoreToExp2);
-                most[c] = now;
-                den[c] *= alpha;
-#pragma unroll
-                for (int d = 0; d < 4; ++d) o[c][d] *= alpha;
-            }
-            const float base = now == -INFINITY ? 0.0f : now * kScoreToExp2;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(s[c][i], kScoreToExp2, -base));
-                den[c] += e;
-                const _Float16 e16 = (_Float16)e;
-                p[c][i / 8][i % 8] = e16;
-                if (kRest) rest[c][i / 8][i % 8] = (_Float16)(e - (float)e16);
+                for (int i = 0; i < 16; ++i) s[w][i] = (bits >> (8 * (i / 4) + i % 4)) & 1u ? s[w][i] : -INFINITY;
             }
         }
+        float mx = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int i = 1; i < 16; ++i) mx = fmaxf(fmaxf(mx, s[0][i]), s[1][i]);
+        mx = halves_max(mx);
+        if (__ballot(mx > most + kAhead / kScoreToExp2) != 0ull) {
+            const float now = fmaxf(most, mx), alpha = most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((most - now) * kScoreToExp2);
+            most = now;
+            den *= alpha;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) o[d] *= alpha;
+        }
+        const float base = most == -INFINITY ? 0.0f : most * kScoreToExp2;
+        half8_t p[4], rest[4];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], kScoreToExp2, -base));
+            den += e;
+            const _Float16 e16 = (_Float16)e;
+            p[i / 8][i % 8] = e16;
+            if (kRest) rest[i / 8][i % 8] = (_Float16)(e - (float)e16);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                const half8_t op = vop[(2 * d + k) * 64];
-#pragma unroll
-                for (int c = 0; c < kCols; ++c) {
-                    o[c][d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, p[c][k], o[c][d], 0, 0, 0);
-                    if (kRest) o[c][d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, rest[c][k], o[c][d], 0, 0, 0);
-                }
+                const half8_t v = op[(k / 2) * (kPair / 2) + kPair / 4 + (2 * d + k % 2) * 64];
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k], o[d], 0, 0, 0);
+                if (kRest) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, rest[k], o[d], 0, 0, 0);
             }
+        keep(which ^ 1);
     }
     // the lane holds dimensions 32 d + 8 (i / 4) + 4 h + i % 4 of its row
-#pragma unroll
-    for (int c = 0; c < kCols; ++c) {
-        den[c] += __shfl_xor(den[c], 32);
-        const int r = (wave * kCols + c) * 32 + n;
-        if (r >= rows) continue;
-        if (a.splits > 1) {
-            const size_t part = ((size_t)at * a.Hkv + hkv) * a.tile_rows * a.splits + (size_t)r * a.splits + split;
-            const size_t all = (size_t)tiles * a.Hkv * a.tile_rows * a.splits;
-            float* to = a.lay.partial + part * kGroup + 4 * h;
-#pragma unroll
-            for (int d = 0; d < 4; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) *reinterpret_cast<float4_t*>(to + 32 * d + 8 * i) = float4_t{o[c][d][4 * i], o[c][d][4 * i + 1], o[c][d][4 * i + 2], o[c][d][4 * i + 3]};
-            if (h == 0) {
-                a.lay.partial[all * kGroup + part * 2] = most[c] * 0.08838834764831845f;
-                a.lay.partial[all * kGroup + part * 2 + 1] = den[c];
-            }
-            continue;
-        }
-        const float one = den[c] > 0.0f ? 1.0f / den[c] : 0.0f;
+    den += __shfl_xor(den, 32);
+    const int own = wave * 32 + n;
+    if (own >= rows) return;
+    if (a.splits > 1) {
+        const size_t part = (((size_t)at * a.Hkv + hkv) * a.tile_rows + own) * a.splits + split, all = (size_t)tiles * a.Hkv * a.tile_rows * a.splits;
+        float* to = a.lay.partial + part * kGroup + 4 * h;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float4_t v = float4_t{o[c][d][4 * i], o[c][d][4 * i + 1], o[c][d][4 * i + 2], o[c][d][4 * i + 3]} * one;
-                const size_t to = out_at[c] + 32 * d + 8 * i + 4 * h;
-                if (a.half) {
-                    typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
-                    *reinterpret_cast<half4_t*>(static_cast<_Float16*>(a.out) + to) = half4_t{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
-                } else {
-                    *reinterpret_cast<float4_t*>(static_cast<float*>(a.out) + to) = v;
-                }
-            }
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<float4_t*>(to + 32 * d + 8 * i) = float4_t{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+        if (h == 0) {
+            a.lay.partial[all * kGroup + part * 2] = most * 0.08838834764831845f;
+            a.lay.partial[all * kGroup + part * 2 + 1] = den;
+        }
+        return;
     }
+    const float one = den > 0.0f ? 1.0f / den : 0.0f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4_t v = float4_t{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]} * one;
+            const size_t to = out_at + 32 * d + 8 * i + 4 * h;
+            if (!kRest) {
+                typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
+                *reinterpret_cast<half4_t*>(static_cast<_Float16*>(a.out) + to) = half4_t{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
+            } else {
+                *reinterpret_cast<float4_t*>(static_cast<float*>(a.out) + to) = v;
+            }
+        }
 }
 
 // merges the token ranges of a row: grid (tiles that there may be * Hkv, rows of a tile), 128 threads
@@ -734,7 +757,7 @@ __global__ __launch_bounds__(kGroup) void attend_tiles_merge_kernel(TileArgs a) 
 
 // ---- host side -----------------------------------------------------------------------------------------------------------
 struct Plan {
-    int few, tiles, splits;                      // rows taken 16 at a time: up to how many of a sequence; tiles of 16; ranges of the tokens
+    int few, few_rows, splits;                   // sequences with up to `few` rows are taken on the way: the kernel's rows, ranges of the tokens
     int wide_tiles, tile_rows, wide_splits, units;  // the others: tiles that there may be, their rows, ranges of the tokens, units in the workspace
     size_t few_bytes, bytes;                     // of the workspace
 };
@@ -744,17 +767,19 @@ Plan plan_of(int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int6
     max_new = std::min(max_new, n_tokens);
     const int grp = Hq / Hkv;
     const long long rows = (long long)max_new * grp;
-    const bool all = rows > kFewRows && (long long)max_new * B == n_tokens;  // every sequence has as many rows
-    p.few = all ? 0 : kFewRows;
+    const bool wide = rows > kFewRows, all = wide && (long long)max_new * B == n_tokens;  // every sequence has as many rows
+    // Beside chunks, what is taken on the way is sequences with a token each, in the kernel that suits those.
+    const long long few = wide ? grp : rows;
+    p.few_rows = few <= 8 ? 8 : few <= 16 ? 16 : kFewRows;
+    p.few = all ? 0 : (int)few;
     if (!all) {
-        p.tiles = (int)((std::min<long long>(rows, kFewRows) + kGqaMaxGroup - 1) / kGqaMaxGroup);
-        const long long wgs = (long long)B * Hkv * p.tiles;
+        const long long wgs = (long long)B * Hkv;
         p.splits = (int)std::min<long long>(std::min<long long>(std::max<long long>(1, cus / wgs), ((long long)max_kv + 255) / 256), 256);
-        p.few_bytes = p.splits > 1 ? round_up((size_t)wgs * kGqaMaxGroup * p.splits * (kGroup + 2) * sizeof(float)) : 0;
+        p.few_bytes = p.splits > 1 ? round_up((size_t)wgs * p.few_rows * p.splits * (kGroup + 2) * sizeof(float)) : 0;
     }
     p.bytes = p.few_bytes;
-    if (rows > kFewRows) {
-        p.tile_rows = 128;
+    if (wide) {
+        p.tile_rows = 32 * ((long long)n_tokens * grp / 256 * Hkv >= cus ? 8 : 4);
         const long long many = std::min<long long>(B, (long long)n_tokens * grp / ((long long)p.few + 1));  // sequences with more rows than `few`
         p.wide_tiles = (int)((long long)n_tokens * grp / p.tile_rows + many);
         const long long units = std::min<long long>((std::min<long long>(total_kv, (long long)many * max_kv)) / kUnitBlocks + many, 0x7FFFFFFF);
@@ -804,7 +829,7 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
     hipStream_t st = static_cast<hipStream_t>(stream);
     PagedArgs args{mk->dev, mv->dev, q, static_cast<const uint4*>(k_blocks), k_meta, static_cast<const uint4*>(v_blocks), v_meta, page_table, q_start, kv_len,
                    out, static_cast<float*>(workspace), q_stride, mk->S, mv->S, B, Hq, Hkv, n_tokens, n_pages, shift, max_pages, max_kv,
-                   plan.tiles, 0, 0, 0, 0, out_half, plan.few};
+                   0, 0, 0, 0, out_half, plan.few};
     if (plan.wide_tiles > 0) {
         char* at = static_cast<char*>(workspace) + plan.few_bytes;
         const auto part = [&](size_t bytes) {
@@ -835,18 +860,22 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
                     : (lv ? expand(attend_expand_kernel<false, true>) : expand(attend_expand_kernel<false, false>));
         if (rc != ECCO_OK) return rc;
         const dim3 grid((unsigned)plan.wide_tiles * Hkv, plan.wide_splits);
-        if (out_half) hipLaunchKernelGGL((attend_tiles_kernel<4, 1, false>), grid, dim3(256), 0, st, t);
-        else hipLaunchKernelGGL((attend_tiles_kernel<4, 1, true>), grid, dim3(256), 0, st, t);
+        const auto products = [&](auto waves) {
+            constexpr int kWaves = decltype(waves)::value;
+            if (out_half) hipLaunchKernelGGL((attend_tiles_kernel<kWaves, false>), grid, dim3(kWaves * 64), 0, st, t);
+            else hipLaunchKernelGGL((attend_tiles_kernel<kWaves, true>), grid, dim3(kWaves * 64), 0, st, t);
+        };
+        if (plan.tile_rows == 256) products(std::integral_constant<int, 8>{});
+        else products(std::integral_constant<int, 4>{});
         ECCO_HIP_CHECK(hipGetLastError());
         if (plan.wide_splits > 1) {
             hipLaunchKernelGGL(attend_tiles_merge_kernel, dim3((unsigned)plan.wide_tiles * Hkv, plan.tile_rows), dim3(kGroup), 0, st, t);
             ECCO_HIP_CHECK(hipGetLastError());
         }
     }
-    if (plan.tiles == 0) return ECCO_OK;
-    const int rows = (int)std::min<long long>(kGqaMaxGroup, (long long)std::min(max_new, n_tokens) * (Hq / Hkv));
+    if (plan.few == 0) return ECCO_OK;
     const int units = (units_of(max_kv) + plan.splits - 1) / plan.splits;
-    const GqaPlan g = gqa_plan(mk->S, lk, mv->S, lv, rows, (size_t)B * Hkv * plan.tiles * plan.splits, units, cus);
+    const GqaPlan g = rows_plan(mk->S, lk, mv->S, lv, plan.few, (size_t)B * Hkv * plan.splits, units, cus);
     args.table_words = g.table_words;
     args.both = g.both;
     args.span = g.span;
@@ -854,19 +883,22 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
     const auto launch = [&](auto kernel) -> int {
         const int rc = allow_lds(kernel, dev_id, g.lds);
         if (rc != ECCO_OK) return rc;
-        hipLaunchKernelGGL(kernel, dim3(B * Hkv, plan.splits, plan.tiles), dim3(g.waves * 64), g.lds, st, args);
+        hipLaunchKernelGGL(kernel, dim3(B * Hkv, plan.splits), dim3(g.waves * 64), g.lds, st, args);
         ECCO_HIP_CHECK(hipGetLastError());
         return ECCO_OK;
     };
-    const auto pick = [&](auto wide) -> int {
-        constexpr bool kWide = decltype(wide)::value;
-        if (lk) return lv ? launch(attend_rows_kernel<true, true, kWide, 12>) : launch(attend_rows_kernel<true, false, kWide, 12>);
-        if (lv) return launch(attend_rows_kernel<false, true, kWide, 12>);
-        return g.waves == 8 ? launch(attend_rows_kernel<false, false, kWide, 8>) : launch(attend_rows_kernel<false, false, kWide, 12>);
+    const auto pick = [&](auto row_tag) -> int {
+        constexpr int kRows = decltype(row_tag)::value;
+        constexpr int kLongWaves = kRows == kFewRows ? 8 : 12;
+        if (lk) return lv ? launch(attend_rows_kernel<true, true, kRows, kLongWaves>) : launch(attend_rows_kernel<true, false, kRows, kLongWaves>);
+        if (lv) return launch(attend_rows_kernel<false, true, kRows, 12>);
+        if constexpr (kRows <= 16)
+            if (g.waves == 8) return launch(attend_rows_kernel<false, false, kRows, 8>);
+        return launch(attend_rows_kernel<false, false, kRows, 12>);
     };
-    const int rc = rows > 8 ? pick(std::true_type{}) : pick(std::false_type{});
+    const int rc = plan.few_rows == 8 ? pick(std::integral_constant<int, 8>{}) : plan.few_rows == 16 ? pick(std::integral_constant<int, 16>{}) : pick(std::integral_constant<int, kFewRows>{});
     if (rc != ECCO_OK || plan.splits == 1) return rc;
-    hipLaunchKernelGGL(attend_rows_merge_kernel, dim3(B * Hkv, rows, plan.tiles), dim3(kGroup), 0, st, args, plan.splits);
+    hipLaunchKernelGGL(attend_rows_merge_kernel, dim3(B * Hkv, plan.few), dim3(kGroup), 0, st, args, plan.few_rows, plan.splits);
     ECCO_HIP_CHECK(hipGetLastError());
     return ECCO_OK;
 }
