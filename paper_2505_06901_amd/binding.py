@@ -345,81 +345,89 @@ def ecco_act_decode(blocks, dst=None):
 
 
 # ---- the compressed cache in pages (include/ecco_paged.h) ---------------------------------------------------------
-def _int32(*tensors):
+# A decoding step makes three of these calls, and what they launch takes 5 to 30 us: each looks at a tensor once.
+_types = ()  # (torch.int32, torch.float16, torch.float32), looked up with the first call
+
+
+def _torch_types():
+    global _types
     import torch
-    for t in tensors:
-        assert t is None or t.dtype == torch.int32, "int32 tensors expected"
+    _types = (torch.int32, torch.float16, torch.float32)
+    return _types
 
 
-def _rows(x):
-    """(pointer, values from row to row) of a CUDA FP16 tensor [rows, heads, 128] whose rows are contiguous."""
-    import torch
-    assert x.is_cuda and x.dtype == torch.float16 and x.dim() == 3 and x.shape[2] == GROUP
-    assert x.numel() == 0 or x[0].is_contiguous(), "a row's heads must be contiguous"
-    return x.data_ptr(), (x.stride(0) if x.shape[0] > 1 else x.shape[1] * GROUP)
+def _int32(t, n: int) -> int:
+    """Device pointer of a contiguous CUDA int32 tensor of at least n elements."""
+    assert t.dtype is (_types or _torch_types())[0] and t.is_cuda and t.is_contiguous() and t.numel() >= n, "contiguous CUDA int32 tensors expected"
+    return t.data_ptr()
 
 
-def _pool(k_blocks, k_meta, v_blocks, v_meta):
-    """(pages, heads, tokens of a page) of a pool's tensors."""
-    import torch
-    assert k_meta.dim() == 3 and v_meta.shape == k_meta.shape, "meta words are [n_pages, heads, page_tokens]"
-    for blocks in (k_blocks, v_blocks):
-        assert blocks.dtype == torch.uint8 and blocks.numel() == k_meta.numel() * BLOCK_BYTES, "64 bytes per meta word"
-    assert k_meta.element_size() == 4 and v_meta.element_size() == 4
-    return k_meta.shape
+def _rows(x, n: int, heads: int) -> int:
+    """Device pointer of a CUDA FP16 tensor [n, heads, 128] whose rows are contiguous, at any distance from each other."""
+    assert x.dtype is (_types or _torch_types())[1] and x.is_cuda and x.shape == (n, heads, GROUP), "CUDA FP16 tensors [rows, heads, 128] expected"
+    stride = x.stride()
+    assert stride[2] == 1 and (stride[1] == GROUP or heads == 1), "a row's heads must be contiguous"
+    return x.data_ptr()
+
+
+def _row_stride(x, n: int, heads: int) -> int:
+    return x.stride(0) if n > 1 else heads * GROUP
+
+
+def _pool(blocks, meta, words: int):
+    """Device pointers of a pool's blocks and of its `words` meta words."""
+    assert blocks.is_cuda and blocks.is_contiguous() and blocks.numel() * blocks.element_size() == words * BLOCK_BYTES, "contiguous, 64 bytes per meta word"
+    return blocks.data_ptr(), _int32(meta, words)
 
 
 def ecco_kv_pages_take(seq_len, new_len, page_table, free_pages, free_count, page_tokens: int, n_tokens: int, free_left=None, q_start=None,
                        kv_len=None, slots=None):
     """seq_len, new_len int32 [B]; page_table int32 [B, max_pages], updated in place; free_pages int32 [n_pages]; free_count int32 [1], updated
     in place unless free_left is another tensor.  Returns (q_start [B + 1], kv_len [B], slots [n_tokens])."""
-    import torch
     B, max_pages = page_table.shape
-    assert seq_len.numel() == B and new_len.numel() == B
-    q_start = torch.empty((B + 1,), dtype=torch.int32, device=page_table.device) if q_start is None else q_start
-    kv_len = torch.empty((B,), dtype=torch.int32, device=page_table.device) if kv_len is None else kv_len
-    slots = torch.empty((n_tokens,), dtype=torch.int32, device=page_table.device) if slots is None else slots
-    free_left = free_count if free_left is None else free_left
-    _int32(seq_len, new_len, page_table, free_pages, free_count, free_left, q_start, kv_len, slots)
-    assert q_start.numel() >= B + 1 and kv_len.numel() >= B and slots.numel() >= n_tokens
-    _check(lib().ecco_kv_pages_take(_dp(seq_len), _dp(new_len), B, page_tokens, max_pages, _dp(page_table), _dp(free_pages), _dp(free_count),
-                                    _dp(free_left), free_pages.numel(), n_tokens, _dp(q_start), _dp(kv_len), _dp(slots), _stream()), "ecco_kv_pages_take")
+    if q_start is None or kv_len is None or slots is None:
+        import torch
+        new = lambda t, n: torch.empty((n,), dtype=torch.int32, device=page_table.device) if t is None else t  # noqa: E731
+        q_start, kv_len, slots = new(q_start, B + 1), new(kv_len, B), new(slots, n_tokens)
+    count = _int32(free_count, 1)
+    n_pages = free_pages.numel()
+    _check(lib().ecco_kv_pages_take(_int32(seq_len, B), _int32(new_len, B), B, page_tokens, max_pages, _int32(page_table, 0), _int32(free_pages, n_pages), count,
+                                    count if free_left is None else _int32(free_left, 1), n_pages, n_tokens, _int32(q_start, B + 1), _int32(kv_len, B),
+                                    _int32(slots, n_tokens), _stream()), "ecco_kv_pages_take")
     return q_start, kv_len, slots
 
 
 def ecco_kv_pages_release(seq_len, keep_len, page_table, free_pages, free_count, page_tokens: int, free_left=None):
-    """Pages of the tokens keep_len .. seq_len go back onto free_pages; free_count is updated in place unless free_left is another tensor."""
+    """Pages of the tokens keep_len .. seq_len go back onto free_pages; free_count is updated in place unless free_left is another tensor.
+    Returns the tensor with the new count."""
     B, max_pages = page_table.shape
-    assert seq_len.numel() == B and keep_len.numel() == B
     free_left = free_count if free_left is None else free_left
-    _int32(seq_len, keep_len, page_table, free_pages, free_count, free_left)
-    _check(lib().ecco_kv_pages_release(_dp(seq_len), _dp(keep_len), B, page_tokens, max_pages, _dp(page_table), _dp(free_pages), _dp(free_count),
-                                       _dp(free_left), free_pages.numel(), _stream()), "ecco_kv_pages_release")
+    n_pages = free_pages.numel()
+    _check(lib().ecco_kv_pages_release(_int32(seq_len, B), _int32(keep_len, B), B, page_tokens, max_pages, _int32(page_table, 0), _int32(free_pages, n_pages),
+                                       _int32(free_count, 1), _int32(free_left, 1), n_pages, _stream()), "ecco_kv_pages_release")
     return free_left
 
 
-def _append_paged(name: str, mk: Model, mv: Model, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots):
-    n_pages, H, page_tokens = _pool(k_blocks, k_meta, v_blocks, v_meta)
-    assert k_new.shape == v_new.shape and k_new.shape[1] == H and slots.numel() >= k_new.shape[0]
-    _int32(slots)
-    (k, k_stride), (v, v_stride) = _rows(k_new), _rows(v_new)
-    _check(getattr(lib(), name)(mk.handle, mv.handle, k, v, k_stride, v_stride, _dp(k_blocks), _dp(k_meta), _dp(v_blocks), _dp(v_meta), _dp(slots),
-                                k_new.shape[0], H, n_pages, page_tokens, _stream()), name)
+def _append_paged(call, name: str, mk: Model, mv: Model, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots):
+    n_pages, H, page_tokens = k_meta.shape
+    n, words = k_new.shape[0], n_pages * H * page_tokens
+    _check(call(mk.handle, mv.handle, _rows(k_new, n, H), _rows(v_new, n, H), _row_stride(k_new, n, H), _row_stride(v_new, n, H),
+                *_pool(k_blocks, k_meta, words), *_pool(v_blocks, v_meta, words), _int32(slots, n), n, H, n_pages, page_tokens, _stream()), name)
 
 
 def ecco_kv_append_paged(mk: Model, mv: Model, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots):
     """k_new, v_new: CUDA FP16 [n_tokens, H, 128], views into a wider tensor allowed; pools [n_pages, H, page_tokens]; slots int32 [n_tokens]."""
-    _append_paged("ecco_kv_append_paged", mk, mv, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots)
+    _append_paged(lib().ecco_kv_append_paged, "ecco_kv_append_paged", mk, mv, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots)
 
 
 def ecco_kv_append_paged_minmax(mk: Model, mv: Model, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots):
     """As ecco_kv_append_paged, with the min/max pattern selector."""
-    _append_paged("ecco_kv_append_paged_minmax", mk, mv, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots)
+    _append_paged(lib().ecco_kv_append_paged_minmax, "ecco_kv_append_paged_minmax", mk, mv, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots)
 
 
 def ecco_kv_attend_paged_workspace(n_tokens: int, B: int, Hq: int, Hkv: int, max_new: int, max_kv: int, total_kv: int, device: int = 0) -> int:
     """Bytes of the workspace that ecco_kv_attend_paged needs for these sizes."""
-    return int(lib().ecco_kv_attend_paged_workspace(device, n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv))
+    return lib().ecco_kv_attend_paged_workspace(device, n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv)
 
 
 def ecco_kv_attend_paged(mk: Model, mv: Model, q, k_blocks, k_meta, v_blocks, v_meta, page_table, q_start, kv_len, max_new: int, max_kv: int,
@@ -427,24 +435,25 @@ def ecco_kv_attend_paged(mk: Model, mv: Model, q, k_blocks, k_meta, v_blocks, v_
     """q: CUDA FP16 [n_tokens, Hq, 128], a view into a wider tensor allowed; out: FP32 (the default) or FP16 [n_tokens, Hq, 128].  max_new,
     max_kv: at least the most new tokens and the most tokens of a sequence; total_kv: at least the tokens of all of them (default: B times
     max_kv); workspace: uint8 tensor of ecco_kv_attend_paged_workspace bytes."""
-    import torch
-    n_pages, Hkv, page_tokens = _pool(k_blocks, k_meta, v_blocks, v_meta)
+    n_pages, Hkv, page_tokens = k_meta.shape
     B, max_pages = page_table.shape
-    n_tokens, Hq = q.shape[:2]
-    total_kv = B * max_kv if total_kv is None else total_kv
-    _int32(page_table, q_start, kv_len)
-    assert q_start.numel() >= B + 1 and kv_len.numel() >= B
-    if out is None:
-        out = torch.empty((n_tokens, Hq, GROUP), dtype=torch.float32, device=q.device)
-    assert out.shape == q.shape and out.dtype in (torch.float32, torch.float16)
-    if workspace is None:
-        size = ecco_kv_attend_paged_workspace(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv, q.device.index or 0)
-        workspace = torch.empty((size,), dtype=torch.uint8, device=q.device) if size else None
-    ptr, stride = _rows(q)
-    _check(lib().ecco_kv_attend_paged(mk.handle, mv.handle, ptr, stride, _dp(k_blocks), _dp(k_meta), _dp(v_blocks), _dp(v_meta), _dp(page_table),
-                                      _dp(q_start), _dp(kv_len), n_tokens, B, Hq, Hkv, n_pages, page_tokens, max_pages, max_new, max_kv, total_kv,
-                                      _dp(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _dp(out),
-                                      int(out.dtype == torch.float16), _stream()), "ecco_kv_attend_paged")
+    n_tokens, Hq, _ = q.shape
+    words = n_pages * Hkv * page_tokens
+    if total_kv is None:
+        total_kv = B * max_kv
+    if out is None or workspace is None:
+        import torch
+        if out is None:
+            out = torch.empty((n_tokens, Hq, GROUP), dtype=torch.float32, device=q.device)
+        if workspace is None:
+            size = ecco_kv_attend_paged_workspace(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv, q.device.index or 0)
+            workspace = torch.empty((size,), dtype=torch.uint8, device=q.device)
+    half = out.dtype is (_types or _torch_types())[1]
+    assert out.shape == q.shape and (half or out.dtype is _types[2]), "FP32 or FP16 outputs like q"
+    _check(lib().ecco_kv_attend_paged(mk.handle, mv.handle, _rows(q, n_tokens, Hq), _row_stride(q, n_tokens, Hq), *_pool(k_blocks, k_meta, words),
+                                      *_pool(v_blocks, v_meta, words), _int32(page_table, 0), _int32(q_start, B + 1), _int32(kv_len, B), n_tokens, B, Hq, Hkv,
+                                      n_pages, page_tokens, max_pages, max_new, max_kv, total_kv, _dp(workspace), workspace.numel() * workspace.element_size(),
+                                      _dp(out), int(half), _stream()), "ecco_kv_attend_paged")
     return out
 
 

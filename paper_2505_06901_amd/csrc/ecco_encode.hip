@@ -59,7 +59,8 @@ struct AppendIo {
         return t >= 0 && t < t_max;
     }
 };
-// rows of new tokens: group (row, h) goes to the row's slot in head h of its page, if the slot is one of the pool's
+// Rows of new tokens: group (row, h) goes to the row's slot in head h of its page, if the slot is one of the pool's.  A batch is neighbouring rows
+// of one head, not neighbouring heads of a row: their slots are as a rule neighbours too, and the blocks fill whole lines.
 struct PagedIo {
     static constexpr bool kDense = false;
     const uint32_t* src;
@@ -67,27 +68,48 @@ struct PagedIo {
     uint32_t* meta;
     const int32_t* slots;
     int64_t stride;  // words from row to row
-    int n, heads, shift;
+    int rows, heads, shift;
     uint32_t n_slots;
-    __device__ __forceinline__ size_t groups() const { return (size_t)n; }
-    __device__ __forceinline__ bool place(size_t i, size_t& at) const {
-        if (i >= (size_t)n) return false;
-        const uint32_t row = (uint32_t)i / (uint32_t)heads, h = (uint32_t)i - row * (uint32_t)heads, slot = (uint32_t)slots[row];
+    __host__ __device__ size_t batches(int batch) const { return (size_t)((rows - 1) / batch + 1) * heads; }
+    // the slot of row `local` of batch b: asked for ahead of `place`, which waits for it
+    template <int kBatch>
+    __device__ __forceinline__ uint32_t slot(size_t b, int local) const {
+        const uint32_t row = (uint32_t)b / (uint32_t)heads * kBatch + (uint32_t)local;
+        return row < (uint32_t)rows ? (uint32_t)slots[row] : ~0u;
+    }
+    __device__ __forceinline__ bool place(size_t b, uint32_t slot, size_t& at) const {
+        const uint32_t h = (uint32_t)b % (uint32_t)heads;
         at = (((size_t)(slot >> shift) * heads + h) << shift) + (slot & ((1u << shift) - 1u));
         return slot < n_slots;
     }
     template <int kBatch>
     __device__ __forceinline__ void load(RowValues& v, size_t b, int local, int l) const {
-        const uint32_t i = (uint32_t)min(b * kBatch + (uint32_t)local, (size_t)(n - 1)), row = i / (uint32_t)heads, h = i - row * (uint32_t)heads;
+        const uint32_t block = (uint32_t)b / (uint32_t)heads, h = (uint32_t)b - block * (uint32_t)heads;
+        const uint32_t row = min(block * kBatch + (uint32_t)local, (uint32_t)rows - 1u);  // (also of a batch behind the last)
         const u32x4_dword t = *reinterpret_cast<const u32x4_dword*>(src + (size_t)row * stride + (h * kRowLanes + l) * 4);
         v.x[0] = t.x; v.x[1] = t.y; v.x[2] = t.z; v.x[3] = t.w;
     }
 };
-// the values of group `local` of batch b
+// the groups of a source in batches: how many there are, the values of one, its place
+template <int kBatch, class Io>
+__device__ __forceinline__ size_t batches_of(const Io& io) {
+    if constexpr (std::is_same<Io, PagedIo>::value) return io.batches(kBatch);
+    else return (io.groups() + kBatch - 1) / kBatch;
+}
 template <int kBatch, class Io>
 __device__ __forceinline__ void load_group(RowValues& v, const Io& io, size_t b, int local, int l) {
     if constexpr (std::is_same<Io, PagedIo>::value) io.template load<kBatch>(v, b, local, l);
     else load_values<kBatch>(v, io.values(), io.groups(), b, local, l);
+}
+template <int kBatch, class Io>
+__device__ __forceinline__ uint32_t slot_of(const Io& io, size_t b, int local) {
+    if constexpr (std::is_same<Io, PagedIo>::value) return io.template slot<kBatch>(b, local);
+    else return 0u;
+}
+template <class Io>
+__device__ __forceinline__ bool place_group(const Io& io, size_t g, size_t b, uint32_t slot, size_t& at) {  // g: the group, of batch b
+    if constexpr (std::is_same<Io, PagedIo>::value) return io.place(b, slot, at);
+    else return io.place(g, at);
 }
 template <class Io>
 struct Job {  // one model and the groups it encodes; blockIdx.y picks one of two (keys and values)
@@ -211,7 +233,7 @@ __global__ __launch_bounds__(kSearchThreads) __attribute__((amdgpu_waves_per_eu(
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const SearchLds L = search_lds<search_over(kTiles)>(smem + S * kTableWords, kTiles);
     uint32_t* hist = L.hist + (wave * kWaveRows + row) * kHistStride;
-    const size_t batches = (io.groups() + kSearchBatch - 1) / kSearchBatch;
+    const size_t batches = batches_of<kSearchBatch>(io);
     RowValues v;
     load_group<kSearchBatch>(v, io, blockIdx.x, wave * kWaveRows + row, l);
     Coefs<kTiles> C;
@@ -296,10 +318,11 @@ __global__ __launch_bounds__(kSearchThreads) __attribute__((amdgpu_waves_per_eu(
         asm volatile("" : "+v"(last));
         const int place = last & 15, group = wave * kWaveRows + (last >> 4);
         load_group<kSearchBatch>(v, io, b + gridDim.x, group, place);
+        const uint32_t slot = slot_of<kSearchBatch>(io, b, group);
         uint32_t mw;
         const uint32_t word = pack_row<kLong>(T.enc + pattern * (kK * 4u), L.hist + group * kHistStride, idx, place, smax, pattern, mw);
         size_t at;
-        if (io.place(b * kSearchBatch + (uint32_t)group, at)) {
+        if (place_group(io, b * kSearchBatch + (uint32_t)group, b, slot, at)) {
             io.blocks[at * kBlockWords + place] = word;
             if (place == 0) io.meta[at] = mw;
         }
@@ -378,7 +401,7 @@ __global__ __launch_bounds__(kFewThreads) void encode_few_kernel(Job<Io> j0, Job
     const int tid = threadIdx.x, l = tid & 15, row = tid >> 4;
     const size_t g = blockIdx.x;
     size_t at;
-    if (!io.place(g, at)) return;  // uniform
+    if (!place_group(io, g, g, slot_of<1>(io, g, 0), at)) return;  // uniform
     RowValues v;
     load_group<1>(v, io, g, 0, l);
     static_assert(kMaxS * kK / 4 <= kFewThreads, "a piece of each table per thread");
@@ -509,7 +532,7 @@ __global__ __launch_bounds__(kMinmaxThreads) void encode_minmax_kernel(Job<Io> j
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t* ends = smem + minmax_table_words(S, kFine);
     uint32_t* image = ends + S + (wave * kWaveRows + row) * kImageStride;
-    const size_t batches = (io.groups() + kMinmaxBatch - 1) / kMinmaxBatch;
+    const size_t batches = batches_of<kMinmaxBatch>(io);
     RowValues v, next;
     load_group<kMinmaxBatch>(v, io, blockIdx.x, wave * kWaveRows + row, l);
     const EncTables T = stage_enc_tables<kMinmaxThreads, kFine>(smem, job.dev, S);
@@ -520,6 +543,7 @@ __global__ __launch_bounds__(kMinmaxThreads) void encode_minmax_kernel(Job<Io> j
     __syncthreads();
     for (size_t b = blockIdx.x; b < batches; b += gridDim.x) {
         const size_t g = b * kMinmaxBatch + wave * kWaveRows + row;
+        const uint32_t slot = slot_of<kMinmaxBatch>(io, b, wave * kWaveRows + row);
         load_group<kMinmaxBatch>(next, io, b + gridDim.x, wave * kWaveRows + row, l);
         const half2_t ends2 = row_ends(v);
         const uint32_t both = __builtin_bit_cast(uint32_t, ends2) & 0x7FFF7FFFu, smax = max(both & 0xFFFFu, both >> 16);
@@ -544,7 +568,7 @@ __global__ __launch_bounds__(kMinmaxThreads) void encode_minmax_kernel(Job<Io> j
         uint32_t mw;
         const uint32_t word = pack_row<kLong>(T.enc + pattern * (kK * 4u), image, idx, l, smax, pattern, mw);
         size_t at;
-        if (io.place(g, at)) {
+        if (place_group(io, g, b, slot, at)) {
             ecco_stream::store<kStream>(io.blocks + at * kBlockWords + l, word);
             if (l == 0) io.meta[at] = mw;
         }
@@ -572,8 +596,11 @@ int launch_encode(bool minmax, const ecco_model* m0, const Io& io0, const ecco_m
     const auto run = [&](auto kernel, size_t lds, int batch, int threads, int per_cu) -> int {
         const int rc = allow_lds(kernel, m0->device, lds);
         if (rc != ECCO_OK) return rc;
-        const size_t wgs = (groups + batch - 1) / batch;
-        const dim3 grid((unsigned)std::min<size_t>(wgs, (size_t)cu_count(m0->device) * per_cu), jobs);
+        size_t wgs = (groups + batch - 1) / batch;
+        if constexpr (std::is_same<Io, PagedIo>::value) wgs = io0.batches(batch);
+        // (what a workgroup stages is spread over more batches if the jobs of a chunk share the compute units)
+        const size_t most = (size_t)cu_count(m0->device) * per_cu / (std::is_same<Io, PagedIo>::value ? jobs : 1);
+        const dim3 grid((unsigned)std::min<size_t>(wgs, most), jobs);
         hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, st, j0, j1);
         ECCO_HIP_CHECK(hipGetLastError());
         return ECCO_OK;
@@ -647,8 +674,8 @@ int kv_append_paged_common(bool minmax, const ecco_model* mk, const ecco_model* 
     if (n_tokens == 0) return ECCO_OK;
     const int shift = __builtin_ctz((unsigned)page_tokens);
     const uint32_t n_slots = (uint32_t)n_pages << shift;
-    const PagedIo k{reinterpret_cast<const uint32_t*>(k_new), static_cast<uint32_t*>(k_blocks), k_meta, slots, k_stride / 2, n_tokens * H, H, shift, n_slots};
-    const PagedIo v{reinterpret_cast<const uint32_t*>(v_new), static_cast<uint32_t*>(v_blocks), v_meta, slots, v_stride / 2, n_tokens * H, H, shift, n_slots};
+    const PagedIo k{reinterpret_cast<const uint32_t*>(k_new), static_cast<uint32_t*>(k_blocks), k_meta, slots, k_stride / 2, n_tokens, H, shift, n_slots};
+    const PagedIo v{reinterpret_cast<const uint32_t*>(v_new), static_cast<uint32_t*>(v_blocks), v_meta, slots, v_stride / 2, n_tokens, H, shift, n_slots};
     return launch_encode(minmax, mk, k, mv, v, (size_t)n_tokens * H, 2, stream);
 }
 
