@@ -29,11 +29,13 @@ struct PagedArgs {
     const int32_t* q_start;
     const int32_t* kv_len;
     void* out;
-    float* ws;
+    float* ws;        // partial results of ranges
+    int32_t* ranges;  // [B] (first, count) of the sequences' ranges
     int64_t q_stride;
     int Sk, Sv, B, Hq, Hkv, n_tokens, n_pages, shift, max_pages, max_kv;
     int table_words, both, span, step, half;
-    int few;  // rows of a sequence and key/value head up to which it is taken 16 at a time
+    int few;       // rows of a sequence and key/value head up to which it is decoded on the way
+    int cut, cus;  // whether sequences are cut into ranges, and for how many workgroups at once
 };
 
 // The arguments of the running kernel, read again: what the loops need of them once per unit would otherwise take scalar registers
@@ -57,6 +59,7 @@ __device__ __forceinline__ const uint32_t* global_words(const uint32_t* p) { ret
 // What the lengths of the device say of sequence b, within what the host has sized the launch for (no rows if they are none of q's)
 struct Sequence {
     int row0, n_new, kv;  // first row, rows, tokens to read
+    __device__ __forceinline__ Sequence() : row0(0), n_new(0), kv(0) {}
     __device__ __forceinline__ Sequence(args_t* a, int b) {
         const auto* start = in_global(a->q_start);
         row0 = start[b];
@@ -112,8 +115,95 @@ __device__ __forceinline__ UnitLoad load_unit(const UnitPages& p, int hkv, int t
 // scores come from v_mfma_f32_32x32x16_f16 instead: one product per eight values and chain for 32 tokens and up to 32 rows, no half of its operand
 // zeroed, eight query values of one row per lane (lane l decodes chain l / 32 of token l % 32).  With 32 rows the second product runs over two tiles
 // of 16.
-// grid: (B * Hkv, n_splits).  The partial result of a split and row is at index ((sequence and head) * kRows + row) * n_splits + split of the
-// workspace: 128 outputs each, then (maximum, denominator) pairs.
+// grid: ranges of the tokens (Range) that there may be, times Hkv.  Where a sequence has several, the workspace takes 128 outputs of each range
+// and row, then (maximum, denominator) pairs, and a second kernel merges them.
+// Which range of which sequence a workgroup takes.  Ranges are of one length for all sequences, so that one long sequence beside short ones
+// gets many of them: the least length, kRangeLeast units or more, with which all workgroups find a place at once, looked for among 64 (one per
+// lane).  Every wavefront works it out for itself from all the sequences' lengths, a load for up to 64 of them.  (Eight sequences of 690 to
+// 3398 tokens, 8 x 4 heads: 29.3 us with four ranges each, 27.0 us with a workgroup per compute unit, 24.8 us with two; 16 sequences up to 4096 tokens
+// 56.8 us and 50.6 us.)  A merge costs 3 to 4 us, as much as six units more per range: ranges of 4 and 12 units at the least, one sequence of 1000
+// tokens 15.7 and 21.2 us, of 8 units 16.5 us; four of 2000 20.0, 21.6 and 17.1 us.
+constexpr int kRangeLeast = 8;        // units: one for each wavefront
+constexpr int kRangeSequences = 256;  // sequences up to which ranges are cut
+struct Range {
+    int b, hkv;          // sequence, key/value head; b < 0: nothing to do
+    int first, n, index; // ranges of the sequences before this one, of this one, and which of its it is
+    int begin, end;      // tokens
+    Sequence seq;
+};
+template <int kCtrl>
+__device__ __forceinline__ int dpp_int(int v) { return __builtin_amdgcn_mov_dpp(v, kCtrl, 0xF, 0xF, true); }
+// sum over the lanes up to and including this one
+__device__ __forceinline__ int wave_scan(int v, int lane) {
+    v += dpp_int<0x111>(v);  // row_shr 1, 2, 4, 8; zeros come in
+    v += dpp_int<0x112>(v);
+    v += dpp_int<0x114>(v);
+    v += dpp_int<0x118>(v);
+    const int a = __builtin_amdgcn_readlane(v, 15), b = a + __builtin_amdgcn_readlane(v, 31), c = b + __builtin_amdgcn_readlane(v, 47);
+    return v + (lane < 16 ? 0 : lane < 32 ? a : lane < 48 ? b : c);
+}
+__device__ __forceinline__ Range find_range(args_t* a, int lane) {
+    const int Hkv = a->Hkv, hkv = blockIdx.x % Hkv, j = blockIdx.x / Hkv;
+    Range r{-1, hkv, 0, 1, 0, 0, 0, Sequence()};
+    if (!a->cut) {  // a workgroup per sequence and head
+        r.b = r.first = j;
+        r.seq = Sequence(a, j);
+        r.end = r.seq.kv;
+        return r;
+    }
+    const int grp = a->Hq / Hkv, B = a->B;
+    constexpr int kChunks = kRangeSequences / 64;
+    int units[kChunks], total = 0;  // of sequence 64 c + l, -1 if it is not one of this kernel's
+    Sequence of[kChunks];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+        units[c] = -1;
+        if (c * 64 >= B) continue;
+        of[c] = Sequence(a, min(c * 64 + lane, B - 1));
+        const int rows = of[c].n_new * grp;
+        if (c * 64 + lane < B && rows > 0 && rows <= a->few) units[c] = of[c].kv > 0 ? units_of(of[c].kv) : 0;
+        total += max(units[c], 0);
+    }
+    total = __builtin_amdgcn_readlane(wave_scan(total, lane), 63);
+    const int least = max(kRangeLeast, (int)ceilf((float)total * (float)Hkv / (float)a->cus * 0.9999f)), step = max(1, least / 16);
+    int length = least + least / 4;
+    if (B <= 32) {
+        const int mine = least + lane * step;
+        const float per = __builtin_amdgcn_rcpf((float)mine);
+        int n = 0;
+        for (int b = 0; b < B; ++b) {
+            const int u = __builtin_amdgcn_readlane(units[0], b);
+            if (u >= 0) n += max(1, (int)((float)(u + mine - 1) * per));
+        }
+        const uint64_t good = __ballot(n * Hkv <= a->cus);
+        if (good != 0ull) length = least + (int)__builtin_ctzll(good) * step;
+    }
+    int before = 0;
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+        if (c * 64 >= B || r.b >= 0) continue;
+        const int n = units[c] < 0 ? 0 : max(1, (units[c] + length - 1) / length), end = wave_scan(n, lane);
+        const uint64_t behind = __ballot(before + end > j);
+        if (behind != 0ull) {
+            const int l = __builtin_ctzll(behind);
+            const auto lane_of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+            r.b = c * 64 + l;
+            r.n = lane_of(n);
+            r.first = before + lane_of(end) - r.n;
+            r.index = j - r.first;
+            r.seq.row0 = lane_of(of[c].row0);
+            r.seq.n_new = lane_of(of[c].n_new);
+            r.seq.kv = lane_of(of[c].kv);
+            const int u = lane_of(units[c]), own = (u + r.n - 1) / r.n;  // the sequence's ranges, alike: at most `length`
+            const auto tokens = [](int n) { return (int)min((int64_t)n * kUnitBlocks, (int64_t)0x7FFFFFFF); };
+            r.begin = tokens(min(r.index * own, u));
+            r.end = tokens(min((r.index + 1) * own, u));
+        }
+        before += __builtin_amdgcn_readlane(end, 63);
+    }
+    return r;
+}
+
 template <bool kLongK, bool kLongV, int kRows, int kWaves>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWaves == 12 ? 3 : kRows > 8 ? 2 : 4))) void attend_rows_kernel(PagedArgs) {
     constexpr int kThreads = kWaves * 64;
@@ -124,15 +214,17 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
     // (one more register than the allocation that bodies of up to 16 rows end in: none of its 64-bit shifts may have its amount in the last one, see build.py)
     if constexpr (kWide) asm volatile("" ::: "v136");
     args_t* const first = fresh_args();
-    const int both = first->both, table_words = first->table_words, Hkv = first->Hkv;
+    const int both = first->both, table_words = first->table_words;
     extern __shared__ __align__(16) uint32_t smem[];
-    const int grp = first->Hq / Hkv, sstride = gqa_score_stride(first->span);
+    const int grp = first->Hq / first->Hkv, sstride = gqa_score_stride(first->span);
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int b = blockIdx.x / Hkv, hkv = blockIdx.x - b * Hkv, split = blockIdx.y;
-    const Sequence seq(first, b);
+    const Range range = find_range(first, lane);
+    const int b = range.b, hkv = range.hkv;
+    if (b < 0) return;  // uniform, ahead of every barrier
+    const Sequence seq = range.seq;
     const int rows = seq.n_new * grp;
-    if (rows <= 0 || rows > first->few) return;  // uniform, ahead of every barrier
+    if (rows <= 0 || rows > first->few) return;
     uint32_t* k_tables = smem;
     uint32_t* wbuf = k_tables + table_words + wave * kUnitWords;
     uint32_t* tile = k_tables + table_words + kWaves * kUnitWords + wave * kTileWords;
@@ -140,11 +232,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
     uint32_t* v_tables = k_tables + (both ? decode_table_words(first->Sk, kLongK) : 0);
     if (lane < kUnitBlocks) wbuf[lane * kStride + kBlockWords] = 0u;
 
-    // the last row's token sees the most: T tokens
-    const int T = max(0, seq.kv), last = T - 1;
-    const int n_splits = gridDim.y;
-    const int64_t per_range = (int64_t)((units_of(max(T, 1)) + n_splits - 1) / n_splits) * kUnitBlocks;
-    const int t_begin = (int)min((int64_t)T, split * per_range), t_end = (int)min((int64_t)T, (split + 1) * per_range);
+    const int last = seq.kv - 1, t_begin = min(range.begin, max(seq.kv, 0)), t_end = min(range.end, max(seq.kv, 0)), n_splits = range.n;
     const int span_max = t_end - t_begin <= first->span ? first->span : first->step;  // a range that one span holds is not cut
     struct Place {
         int lane, n, slice, half, tok;  // n: matrix-core row or column; slice: k slice; half: chain of the lane's token `tok` of the unit
@@ -362,8 +450,10 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
     const int n = P.n, slice = P.slice;
     args_t* const a = fresh_args();
     float* const ws = a->ws;
-    const size_t part = (size_t)blockIdx.x * kRows * n_splits + split;  // of the first row
-    const size_t total = (size_t)gridDim.x * kRows * n_splits;
+    // of the first row; the sequence's and head's rows lie one behind the other, each with its ranges
+    const size_t part = ((size_t)range.first * a->Hkv + (size_t)hkv * n_splits) * kRows + range.index;
+    const size_t total = (size_t)gridDim.x * kRows;
+    if (a->cut && range.index == 0 && hkv == 0 && tid == 0) reinterpret_cast<int2*>(a->ranges)[b] = make_int2(range.first, n_splits);
     float* red = reinterpret_cast<float*>(smem);  // [wavefront][8 tiles][4 slices][16 lanes][4]
     float* state = red + kWaves * 8 * kRedTile;   // [wavefront][16] maxima, [wavefront][16] denominators
 #pragma unroll
@@ -426,14 +516,15 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
 }
 
 // merges the token ranges of a row: grid (B * Hkv, rows that there may be), 128 threads
-__global__ __launch_bounds__(kGroup) void attend_rows_merge_kernel(PagedArgs args, int tile_rows, int n_splits) {
+__global__ __launch_bounds__(kGroup) void attend_rows_merge_kernel(PagedArgs args, int kernel_rows, int n_wgs) {
     args_t* const a = fresh_args();
     const int b = blockIdx.x / args.Hkv, hkv = blockIdx.x - b * args.Hkv, grp = args.Hq / args.Hkv;
+    const int2 ranges = reinterpret_cast<const int2*>(args.ranges)[b];  // (of a sequence that has none, anything: not looked at)
     const Sequence seq(a, b);
     const int r = blockIdx.y, token = r / grp;
-    if (r >= seq.n_new * grp || seq.n_new * grp > args.few) return;
-    const size_t at = ((size_t)blockIdx.x * tile_rows + r) * n_splits, total = (size_t)gridDim.x * tile_rows * n_splits;
-    const float v = merge_splits(args.ws + total * kGroup + at * 2, args.ws + at * kGroup + threadIdx.x, n_splits);
+    if (r >= seq.n_new * grp || seq.n_new * grp > args.few || ranges.y == 1) return;
+    const size_t at = ((size_t)ranges.x * args.Hkv + (size_t)hkv * ranges.y) * kernel_rows + (size_t)r * ranges.y, total = (size_t)n_wgs * kernel_rows;
+    const float v = merge_splits(args.ws + total * kGroup + at * 2, args.ws + at * kGroup + threadIdx.x, ranges.y);
     store_out(a, ((size_t)(seq.row0 + token) * a->Hq + hkv * grp + r - token * grp) * kGroup + threadIdx.x, v);
 }
 
@@ -594,12 +685,19 @@ __device__ __forceinline__ float halves_max(float v) {
     return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
 }
 
-template <int kWaves, bool kRest>
-__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void attend_tiles_kernel(TileArgs a) {
+// Eight wavefronts, 32 rows each, in kGroups groups that each take every kGroups-th pair of units for the tile's rows and add up at the end: what one
+// wavefront of a SIMD waits for, the other one covers, and a workgroup of two groups has half the rows to find work for.
+constexpr int kTileWaves = 8;
+constexpr size_t tiles_lds_bytes(int groups) { return (size_t)groups * 4 * kUnitBytes; }  // two pairs of units per group
+template <int kGroups, bool kRest>
+__global__ __launch_bounds__(kTileWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void attend_tiles_kernel(TileArgs a) {
     constexpr int kPair = 2 * kUnitBytes / 16;            // sixteen-byte pieces of two units
-    constexpr int kPieces = kPair / (kWaves * 64);        // per thread
-    __shared__ __align__(16) u32x4 lds[2][kPair];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+    constexpr int kThreads = kTileWaves * 64 / kGroups;   // of a group
+    constexpr int kPieces = kPair / kThreads;             // per thread
+    extern __shared__ __align__(16) uint32_t smem[];
+    const int tid = threadIdx.x % kThreads, lane = tid & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), group = kGroups == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+    u32x4* const lds = reinterpret_cast<u32x4*>(smem) + group * 2 * kPair;
     const int grp = a.Hq / a.Hkv, hkv = blockIdx.x % a.Hkv, split = blockIdx.y;
     const int tiles = a.lay.tile_start[a.B], at = tiles - 1 - (int)(blockIdx.x / a.Hkv);  // the last tiles have the most tokens: first
     if (at < 0) return;
@@ -633,28 +731,29 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
     const auto load = [&](int u) {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int unit = u + i * (kWaves * 64) / (kPair / 2);
-            piece[i] = src[(int64_t)min(unit, units - 1) * (kUnitBytes / 16) + i * (kWaves * 64) % (kPair / 2) + tid];
+            const int unit = u + i * kThreads / (kPair / 2);
+            piece[i] = src[(int64_t)min(unit, units - 1) * (kUnitBytes / 16) + i * kThreads % (kPair / 2) + tid];
         }
         seen0 = seen[min(u, units - 1)];
         seen1 = seen[min(u + 1, units - 1)];
     };
     const auto keep = [&](int which) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) lds[which][i * (kWaves * 64) + tid] = piece[i];
+        for (int i = 0; i < kPieces; ++i) lds[which * kPair + i * kThreads + tid] = piece[i];
     };
-    static_assert(kWaves * 64 <= kPair / 2, "a round of the threads stays inside a unit");
+    static_assert(kThreads <= kPair / 2, "a round of the threads stays inside a unit");
     if (u_begin < u_end) {
-        load(u_begin);
+        load(u_begin + 2 * group);
         keep(0);
     }
     constexpr float kAhead = 8.0f;
     int which = 0;
-    for (int u = u_begin; u < u_end; u += 2, which ^= 1) {
+    for (int u0 = u_begin; u0 < u_end; u0 += 2 * kGroups, which ^= 1) {
+        const int u = u0 + 2 * group;  // (a group may have nothing left in the last round)
         const uint32_t there0 = seen0, there1 = seen1;
-        load(u + 2);
+        load(u + 2 * kGroups);
         __syncthreads();
-        const half8_t* op = reinterpret_cast<const half8_t*>(lds[which]) + lane;
+        const half8_t* op = reinterpret_cast<const half8_t*>(lds + which * kPair) + lane;
         float16_t s[2];
 #pragma unroll
         for (int k = 0; k < 8; ++k)
@@ -709,6 +808,25 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
             }
         keep(which ^ 1);
     }
+    if constexpr (kGroups == 2) {  // the second group's sums to the first
+        float* const to = reinterpret_cast<float*>(smem) + wave * 66 * 64 + lane;
+        __syncthreads();
+        if (group == 1) {
+            to[0] = most;
+            to[64] = den;
+#pragma unroll
+            for (int i = 0; i < 64; ++i) to[(2 + i) * 64] = o[i / 16][i % 16];
+        }
+        __syncthreads();
+        if (group == 1) return;
+        const float other = to[0], now = fmaxf(most, other);
+        const float mine = most == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((most - now) * kScoreToExp2);
+        const float theirs = other == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((other - now) * kScoreToExp2);
+        most = now;
+        den = den * mine + to[64] * theirs;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) o[i / 16][i % 16] = o[i / 16][i % 16] * mine + to[(2 + i) * 64] * theirs;
+    }
     // the lane holds dimensions 32 d + 8 (i / 4) + 4 h + i % 4 of its row
     den += __shfl_xor(den, 32);
     const int own = wave * 32 + n;
@@ -757,8 +875,8 @@ __global__ __launch_bounds__(kGroup) void attend_tiles_merge_kernel(TileArgs a) 
 
 // ---- host side -----------------------------------------------------------------------------------------------------------
 struct Plan {
-    int few, few_rows, splits;                   // sequences with up to `few` rows are taken on the way: the kernel's rows, ranges of the tokens
-    int wide_tiles, tile_rows, wide_splits, units;  // the others: tiles that there may be, their rows, ranges of the tokens, units in the workspace
+    int few, few_rows, cut, units;               // sequences with up to `few` rows are decoded on the way: the kernel's rows, whether in ranges, units of the longest
+    int wide_tiles, tile_rows, wide_splits, wide_units;  // the others: tiles that there may be, their rows, ranges of the tokens, units in the workspace
     size_t few_bytes, bytes;                     // of the workspace
 };
 constexpr size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -773,19 +891,23 @@ Plan plan_of(int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int6
     p.few_rows = few <= 8 ? 8 : few <= 16 ? 16 : kFewRows;
     p.few = all ? 0 : (int)few;
     if (!all) {
-        const long long wgs = (long long)B * Hkv;
-        p.splits = (int)std::min<long long>(std::min<long long>(std::max<long long>(1, cus / wgs), ((long long)max_kv + 255) / 256), 256);
-        p.few_bytes = p.splits > 1 ? round_up((size_t)wgs * p.few_rows * p.splits * (kGroup + 2) * sizeof(float)) : 0;
+        // Into ranges where there are fewer sequences and heads than compute units, and sequences that one round of the wavefronts does not take
+        p.units = units_of(max_kv);
+        p.cut = B * (long long)Hkv < cus && B <= kRangeSequences && p.units > kRangeLeast;
+        if (p.cut) p.few_bytes = round_up((size_t)B * 8) + round_up((size_t)(B * Hkv + 2 * cus) * p.few_rows * (kGroup + 2) * sizeof(float));
     }
     p.bytes = p.few_bytes;
     if (wide) {
-        p.tile_rows = 32 * ((long long)n_tokens * grp / 256 * Hkv >= cus ? 8 : 4);
+#ifndef TMIN
+#define TMIN 2
+#endif
+        p.tile_rows = (long long)n_tokens * grp / 256 * Hkv >= TMIN * cus ? 256 : 128;
         const long long many = std::min<long long>(B, (long long)n_tokens * grp / ((long long)p.few + 1));  // sequences with more rows than `few`
         p.wide_tiles = (int)((long long)n_tokens * grp / p.tile_rows + many);
         const long long units = std::min<long long>((std::min<long long>(total_kv, (long long)many * max_kv)) / kUnitBlocks + many, 0x7FFFFFFF);
-        p.units = (int)units;
+        p.wide_units = (int)units;
         const long long wgs = (long long)p.wide_tiles * Hkv;
-        p.wide_splits = (int)std::min<long long>(std::min<long long>(std::max<long long>(1, 2 * cus / wgs), ((long long)max_kv + 511) / 512), 64);
+        p.wide_splits = (int)std::min<long long>(std::min<long long>(std::max<long long>(1, cus / wgs), ((long long)max_kv + 511) / 512), 64);
         p.bytes += 2 * round_up(((size_t)B + 1) * 4) + round_up((size_t)units * 4) + (size_t)units * Hkv * kUnitBytes;
         if (p.wide_splits > 1) p.bytes += round_up((size_t)wgs * p.tile_rows * p.wide_splits * (kGroup + 2) * sizeof(float));
     }
@@ -828,8 +950,8 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
     max_kv = std::min(max_kv, max_pages << shift);
     hipStream_t st = static_cast<hipStream_t>(stream);
     PagedArgs args{mk->dev, mv->dev, q, static_cast<const uint4*>(k_blocks), k_meta, static_cast<const uint4*>(v_blocks), v_meta, page_table, q_start, kv_len,
-                   out, static_cast<float*>(workspace), q_stride, mk->S, mv->S, B, Hq, Hkv, n_tokens, n_pages, shift, max_pages, max_kv,
-                   0, 0, 0, 0, out_half, plan.few};
+                   out, reinterpret_cast<float*>(static_cast<char*>(workspace) + round_up((size_t)B * 8)), static_cast<int32_t*>(workspace), q_stride, mk->S, mv->S, B, Hq, Hkv, n_tokens, n_pages, shift, max_pages, max_kv,
+                   0, 0, 0, 0, out_half, plan.few, plan.cut, 0};
     if (plan.wide_tiles > 0) {
         char* at = static_cast<char*>(workspace) + plan.few_bytes;
         const auto part = [&](size_t bytes) {
@@ -840,10 +962,10 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
         TileArgs t{args, {}, plan.tile_rows, plan.wide_splits};
         t.lay.unit_start = reinterpret_cast<int32_t*>(part(((size_t)B + 1) * 4));
         t.lay.tile_start = reinterpret_cast<int32_t*>(part(((size_t)B + 1) * 4));
-        t.lay.seen = reinterpret_cast<uint32_t*>(part((size_t)plan.units * 4));
-        t.lay.operands = reinterpret_cast<uint4*>(part((size_t)plan.units * Hkv * kUnitBytes));
+        t.lay.seen = reinterpret_cast<uint32_t*>(part((size_t)plan.wide_units * 4));
+        t.lay.operands = reinterpret_cast<uint4*>(part((size_t)plan.wide_units * Hkv * kUnitBytes));
         t.lay.partial = reinterpret_cast<float*>(at);
-        t.lay.units = plan.units;
+        t.lay.units = plan.wide_units;
         t.lay.tiles = plan.wide_tiles;
         hipLaunchKernelGGL(attend_layout_kernel, dim3(1), dim3(64), 0, st, t);
         ECCO_HIP_CHECK(hipGetLastError());
@@ -851,7 +973,7 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
             const size_t lds = expand_lds_bytes(std::max(mk->S, mv->S));
             const int rc = allow_lds(kernel, dev_id, lds);
             if (rc != ECCO_OK) return rc;
-            const long long wgs = ((long long)plan.units * Hkv + kExpandWaves - 1) / kExpandWaves;
+            const long long wgs = ((long long)plan.wide_units * Hkv + kExpandWaves - 1) / kExpandWaves;
             hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<long long>(wgs, cus / 2), 2), dim3(kExpandWaves * 64), lds, st, t);
             ECCO_HIP_CHECK(hipGetLastError());
             return ECCO_OK;
@@ -860,13 +982,15 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
                     : (lv ? expand(attend_expand_kernel<false, true>) : expand(attend_expand_kernel<false, false>));
         if (rc != ECCO_OK) return rc;
         const dim3 grid((unsigned)plan.wide_tiles * Hkv, plan.wide_splits);
-        const auto products = [&](auto waves) {
-            constexpr int kWaves = decltype(waves)::value;
-            if (out_half) hipLaunchKernelGGL((attend_tiles_kernel<kWaves, false>), grid, dim3(kWaves * 64), 0, st, t);
-            else hipLaunchKernelGGL((attend_tiles_kernel<kWaves, true>), grid, dim3(kWaves * 64), 0, st, t);
+        const auto products = [&](auto kernel, int groups) -> int {
+            const int rc = allow_lds(kernel, dev_id, tiles_lds_bytes(groups));
+            if (rc != ECCO_OK) return rc;
+            hipLaunchKernelGGL(kernel, grid, dim3(kTileWaves * 64), tiles_lds_bytes(groups), st, t);
+            return ECCO_OK;
         };
-        if (plan.tile_rows == 256) products(std::integral_constant<int, 8>{});
-        else products(std::integral_constant<int, 4>{});
+        if (plan.tile_rows == 256) rc = out_half ? products(attend_tiles_kernel<1, false>, 1) : products(attend_tiles_kernel<1, true>, 1);
+        else rc = out_half ? products(attend_tiles_kernel<2, false>, 2) : products(attend_tiles_kernel<2, true>, 2);
+        if (rc != ECCO_OK) return rc;
         ECCO_HIP_CHECK(hipGetLastError());
         if (plan.wide_splits > 1) {
             hipLaunchKernelGGL(attend_tiles_merge_kernel, dim3((unsigned)plan.wide_tiles * Hkv, plan.tile_rows), dim3(kGroup), 0, st, t);
@@ -874,8 +998,11 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
         }
     }
     if (plan.few == 0) return ECCO_OK;
-    const int units = (units_of(max_kv) + plan.splits - 1) / plan.splits;
-    const GqaPlan g = rows_plan(mk->S, lk, mv->S, lv, plan.few, (size_t)B * Hkv * plan.splits, units, cus);
+    // ranges for as many workgroups as find a place at once
+    args.cus = rows_can_share(mk->S, lk, mv->S, lv, plan.few) ? 2 * cus : cus;
+    const int wgs = B * Hkv + (plan.cut ? args.cus : 0);
+    const int units = plan.cut ? (int)std::min<long long>(plan.units, std::max<long long>(kRangeLeast, ((long long)plan.units * B * Hkv + args.cus - 1) / args.cus)) : plan.units;
+    const GqaPlan g = rows_plan(mk->S, lk, mv->S, lv, plan.few, (size_t)wgs, units, cus, plan.cut);
     args.table_words = g.table_words;
     args.both = g.both;
     args.span = g.span;
@@ -883,7 +1010,7 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
     const auto launch = [&](auto kernel) -> int {
         const int rc = allow_lds(kernel, dev_id, g.lds);
         if (rc != ECCO_OK) return rc;
-        hipLaunchKernelGGL(kernel, dim3(B * Hkv, plan.splits), dim3(g.waves * 64), g.lds, st, args);
+        hipLaunchKernelGGL(kernel, dim3(wgs), dim3(g.waves * 64), g.lds, st, args);
         ECCO_HIP_CHECK(hipGetLastError());
         return ECCO_OK;
     };
@@ -891,14 +1018,14 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
         constexpr int kRows = decltype(row_tag)::value;
         constexpr int kLongWaves = kRows == kFewRows ? 8 : 12;
         if (lk) return lv ? launch(attend_rows_kernel<true, true, kRows, kLongWaves>) : launch(attend_rows_kernel<true, false, kRows, kLongWaves>);
-        if (lv) return launch(attend_rows_kernel<false, true, kRows, 12>);
+        if (lv) return launch(attend_rows_kernel<false, true, kRows, kLongWaves>);
         if constexpr (kRows <= 16)
             if (g.waves == 8) return launch(attend_rows_kernel<false, false, kRows, 8>);
         return launch(attend_rows_kernel<false, false, kRows, 12>);
     };
     const int rc = plan.few_rows == 8 ? pick(std::integral_constant<int, 8>{}) : plan.few_rows == 16 ? pick(std::integral_constant<int, 16>{}) : pick(std::integral_constant<int, kFewRows>{});
-    if (rc != ECCO_OK || plan.splits == 1) return rc;
-    hipLaunchKernelGGL(attend_rows_merge_kernel, dim3(B * Hkv, plan.few), dim3(kGroup), 0, st, args, plan.few_rows, plan.splits);
+    if (rc != ECCO_OK || !plan.cut) return rc;
+    hipLaunchKernelGGL(attend_rows_merge_kernel, dim3(B * Hkv, plan.few), dim3(kGroup), 0, st, args, plan.few_rows, wgs);
     ECCO_HIP_CHECK(hipGetLastError());
     return ECCO_OK;
 }

@@ -121,29 +121,31 @@ inline GqaPlan gqa_plan(int Sk, bool lk, int Sv, bool lv, int grp, size_t wgs, i
 
 // ---- attend_rows_kernel (pages)
 // As GqaPlan for up to `rows` rows (1 to 32), without LDS of its own for the state.  More than 8 rows take more than the 128 registers with which
-// two workgroups share a compute unit; 32 with keys of long codes more than those of twelve wavefronts.
+// two workgroups share a compute unit; 32 with long codes more than those of twelve wavefronts.
 constexpr int kFewRows = 2 * kGqaMaxGroup;
-inline GqaPlan rows_plan(int Sk, bool lk, int Sv, bool lv, int rows, size_t wgs, int units, int cus) {
-    const int wk = decode_table_words(Sk, lk), wv = decode_table_words(Sv, lv), tokens = span_tokens(units);
-    const auto plan = [&](int waves, int lds_words) {
-        const int fixed = waves * (kUnitWords + kTileWords);
-        GqaPlan p;
-        p.waves = waves;
-        const int round = std::min(units, waves) * kUnitBlocks;  // tokens that the wavefronts take at a time
-        p.both = wk + wv + fixed + rows * gqa_score_stride(round) <= lds_words;
-        p.table_words = p.both ? wk + wv : std::max(wk, wv);
-        const int scores = lds_words - p.table_words - fixed;
-        p.span = std::min((scores / rows - 4) & ~(kUnitBlocks - 1), tokens);
-        p.step = p.span < tokens && p.span > round ? p.span - p.span % round : p.span;
-        p.lds = (size_t)std::max(p.table_words + fixed + rows * gqa_score_stride(p.span), gqa_state_words(waves) + waves * 8 * kRedTile) * 4;
-        return p;
-    };
-    if (lk || lv) return plan(lk && rows > kGqaMaxGroup ? 8 : 12, kLdsWords);
-    if (rows <= kGqaMaxGroup / 2) {
-        const GqaPlan two = plan(8, kLdsWords / 2);
-        if (two.both && share_units(wgs, units, cus)) return two;
-    }
-    return plan(units <= 8 && rows <= kGqaMaxGroup ? 8 : 12, kLdsWords);
+inline GqaPlan rows_plan_of(int waves, int lds_words, int wk, int wv, int rows, int units) {
+    const int fixed = waves * (kUnitWords + kTileWords), tokens = span_tokens(units);
+    GqaPlan p;
+    p.waves = waves;
+    const int round = std::min(units, waves) * kUnitBlocks;  // tokens that the wavefronts take at a time
+    p.both = wk + wv + fixed + rows * gqa_score_stride(round) <= lds_words;
+    p.table_words = p.both ? wk + wv : std::max(wk, wv);
+    const int scores = lds_words - p.table_words - fixed;
+    p.span = std::min((scores / rows - 4) & ~(kUnitBlocks - 1), tokens);
+    p.step = p.span < tokens && p.span > round ? p.span - p.span % round : p.span;
+    p.lds = (size_t)std::max(p.table_words + fixed + rows * gqa_score_stride(p.span), gqa_state_words(waves) + waves * 8 * kRedTile) * 4;
+    return p;
+}
+// whether two workgroups of eight wavefronts can share a compute unit
+inline bool rows_can_share(int Sk, bool lk, int Sv, bool lv, int rows) {
+    return !lk && !lv && rows <= kGqaMaxGroup / 2 && rows_plan_of(8, kLdsWords / 2, decode_table_words(Sk, lk), decode_table_words(Sv, lv), rows, 8).both;
+}
+// cut: ranges of one length, of which none outlasts the others where workgroups share.  Otherwise as the contiguous cache's
+inline GqaPlan rows_plan(int Sk, bool lk, int Sv, bool lv, int rows, size_t wgs, int units, int cus, bool cut) {
+    const int wk = decode_table_words(Sk, lk), wv = decode_table_words(Sv, lv);
+    if (lk || lv) return rows_plan_of(rows > kGqaMaxGroup ? 8 : 12, kLdsWords, wk, wv, rows, units);
+    if (rows_can_share(Sk, lk, Sv, lv, rows) && (cut || share_units(wgs, units, cus))) return rows_plan_of(8, kLdsWords / 2, wk, wv, rows, units);
+    return rows_plan_of(units <= 8 && rows <= kGqaMaxGroup ? 8 : 12, kLdsWords, wk, wv, rows, units);
 }
 
 }  // namespace ecco
