@@ -553,26 +553,32 @@ struct Layout {
 struct TileArgs : PagedArgs {
     Layout lay;
     int tile_rows, splits;
+    int layout;  // whether attend_expand_kernel finds the layout by itself
 };
 typedef const __attribute__((address_space(4))) TileArgs tile_args_t;
 
-// One wavefront, 64 sequences at a time.  What does not fit the workspace or the launch, by lengths that the host did not announce, gets no tiles.
+// What sequence 64 c + l of a batch takes, for lane l: units of 32 tokens in the workspace, tiles of rows.  Nothing if it has few rows.
+struct Takes {
+    int units, tiles;
+    Sequence seq;
+    __device__ __forceinline__ Takes(const TileArgs& a, int c, int lane) : units(0), tiles(0) {
+        const int b = 64 * c + lane;
+        seq = Sequence((args_t*)__builtin_amdgcn_kernarg_segment_ptr(), min(b, a.B - 1));
+        const int rows = seq.n_new * (a.Hq / a.Hkv);
+        if (b >= a.B || rows <= a.few) return;
+        units = seq.kv > 0 ? units_of(seq.kv) : 0;
+        tiles = (rows - 1) / a.tile_rows + 1;
+    }
+};
+// One wavefront, 64 sequences at a time.  What does not fit the workspace or the launch, by lengths that the host did not announce, gets no tiles,
+// nor does anything behind it.
 __global__ __launch_bounds__(64) void attend_layout_kernel(TileArgs a) {
-    const int lane = threadIdx.x, grp = a.Hq / a.Hkv;
+    const int lane = threadIdx.x;
     int units = 0, tiles = 0;
     if (lane == 0) a.lay.unit_start[0] = a.lay.tile_start[0] = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const int b = b0 + lane;
-        int u = 0, t = 0;
-        if (b < a.B) {
-            const Sequence s((args_t*)__builtin_amdgcn_kernarg_segment_ptr(), b);
-            const int rows = s.n_new * grp;
-            if (rows > a.few) {
-                u = s.kv > 0 ? units_of(s.kv) : 0;
-                t = (rows - 1) / a.tile_rows + 1;
-            }
-        }
-        int64_t end_u = u, end_t = t;
+    for (int c = 0; c * 64 < a.B; ++c) {
+        const Takes takes(a, c, lane);
+        int64_t end_u = takes.units, end_t = takes.tiles;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const int64_t ou = __shfl_up(end_u, d), ot = __shfl_up(end_t, d);
@@ -584,15 +590,37 @@ __global__ __launch_bounds__(64) void attend_layout_kernel(TileArgs a) {
         const uint64_t good = __ballot(fits);
         const int last = good == ~0ull ? 63 : __builtin_ctzll(~good) - 1;
         const int64_t cap_u = last < 0 ? 0 : __shfl(end_u, max(last, 0)), cap_t = last < 0 ? 0 : __shfl(end_t, max(last, 0));
-        if (b < a.B) {
-            a.lay.unit_start[b + 1] = units + (int)(fits ? end_u : cap_u);
-            a.lay.tile_start[b + 1] = tiles + (int)(fits ? end_t : cap_t);
+        if (64 * c + lane < a.B) {
+            a.lay.unit_start[64 * c + lane + 1] = units + (int)(fits ? end_u : cap_u);
+            a.lay.tile_start[64 * c + lane + 1] = tiles + (int)(fits ? end_t : cap_t);
         }
         units += (int)cap_u;
         tiles += (int)cap_t;
-        if (last < 63) a.lay.units = a.lay.tiles = -1;  // nothing behind it
+        if (last < 63) a.lay.units = a.lay.tiles = -1;
     }
 }
+// The same for up to 64 sequences and sums that an int holds, by any wavefront for itself: the kernel that decodes needs no launch before it then.
+constexpr int kLayoutMost = 1 << 24;  // units, and tiles
+struct Layout64 {
+    int units, end;  // of lane's sequence, and up to and including it
+    Sequence seq;
+    __device__ __forceinline__ Layout64(const TileArgs& a, int lane, bool write) {
+        const Takes takes(a, 0, lane);
+        seq = takes.seq;
+        const int end_u = wave_scan(min(takes.units, kLayoutMost), lane), end_t = wave_scan(min(takes.tiles, kLayoutMost), lane);
+        const uint64_t good = __ballot(end_u <= a.lay.units && end_t <= a.lay.tiles);
+        const int last = good == ~0ull ? 63 : __builtin_ctzll(~good) - 1;
+        const int cap_u = last < 0 ? 0 : __builtin_amdgcn_readlane(end_u, max(last, 0)), cap_t = last < 0 ? 0 : __builtin_amdgcn_readlane(end_t, max(last, 0));
+        units = lane <= last ? takes.units : 0;
+        end = lane <= last ? end_u : cap_u;
+        if (!write) return;
+        if (lane == 0) a.lay.unit_start[0] = a.lay.tile_start[0] = 0;
+        if (lane < a.B) {
+            a.lay.unit_start[lane + 1] = end;
+            a.lay.tile_start[lane + 1] = lane <= last ? end_t : cap_t;
+        }
+    }
+};
 // the sequence that place v of the running sums lies in: the last one that starts at v or before it (and is not empty)
 __device__ __forceinline__ int place_of(const int32_t* start, int B, int v) {
     int lo = 0;
@@ -617,19 +645,30 @@ __device__ __forceinline__ void expand(const TileArgs& a) {
     uint32_t* tile = wbuf + kUnitWords;
     if (lane < kUnitBlocks) wbuf[lane * kStride + kBlockWords] = 0u;
     const TableItems items = load_table_items(dev, S);
+    const Layout64 own(a, lane, a.layout && !kValues && blockIdx.x == 0 && wave == 0);
     build_tables<kLong>(smem, dev, S, items);
     const Tables T = table_pointers(smem, S);
     __syncthreads();
-    const int64_t total = (int64_t)a.lay.unit_start[a.B] * a.Hkv, waves = (int64_t)gridDim.x * kExpandWaves;
+    const int64_t total = (int64_t)(a.layout ? __builtin_amdgcn_readlane(own.end, 63) : a.lay.unit_start[a.B]) * a.Hkv, waves = (int64_t)gridDim.x * kExpandWaves;
     for (int64_t item = (int64_t)blockIdx.x * kExpandWaves + wave; item < total; item += waves) {
-        const int b = __builtin_amdgcn_readfirstlane(place_of(a.lay.unit_start, a.B, (int)(item / a.Hkv)));
-        const int first = a.lay.unit_start[b], units = a.lay.unit_start[b + 1] - first, at = (int)(item - (int64_t)first * a.Hkv);
-        const int hkv = at / units, u = at - hkv * units, t0 = u * kUnitBlocks;
-        const Sequence seq((args_t*)__builtin_amdgcn_kernarg_segment_ptr(), b);
-        const UnitPages pages = unit_pages(b, t0, seq.kv - 1);
+        const int place = (int)(item / a.Hkv);
+        int b, first, units, kv;
+        if (a.layout) {
+            b = (int)__builtin_ctzll(__ballot(own.end > place));  // (place is below the last sum)
+            units = __builtin_amdgcn_readlane(own.units, b);
+            first = __builtin_amdgcn_readlane(own.end, b) - units;
+            kv = __builtin_amdgcn_readlane(own.seq.kv, b);
+        } else {
+            b = __builtin_amdgcn_readfirstlane(place_of(a.lay.unit_start, a.B, place));
+            first = a.lay.unit_start[b];
+            units = a.lay.unit_start[b + 1] - first;
+            kv = Sequence((args_t*)__builtin_amdgcn_kernarg_segment_ptr(), b).kv;
+        }
+        const int at = (int)(item - (int64_t)first * a.Hkv), hkv = at / units, u = at - hkv * units, t0 = u * kUnitBlocks;
+        const UnitPages pages = unit_pages(b, t0, kv - 1);
         bool ok;
         const UnitLoad pre = load_unit<kValues>(pages, hkv, t0, lane, tok, ok);
-        const bool there = ok && t0 + tok < seq.kv;
+        const bool there = ok && t0 + tok < kv;
         const uint32_t mw = there ? pre.meta : 0u;
         if (!kValues && hkv == 0) {
             const uint64_t m = __ballot(there);
@@ -688,7 +727,9 @@ __device__ __forceinline__ float halves_max(float v) {
 // Eight wavefronts, 32 rows each, in kGroups groups that each take every kGroups-th pair of units for the tile's rows and add up at the end: what one
 // wavefront of a SIMD waits for, the other one covers, and a workgroup of two groups has half the rows to find work for.
 constexpr int kTileWaves = 8;
-constexpr size_t tiles_lds_bytes(int groups) { return (size_t)groups * 4 * kUnitBytes; }  // two pairs of units per group
+// two pairs of units per group; at the end 66 words per lane of the second group, and 32 x 68 words per wavefront with rows
+constexpr size_t tiles_lds_bytes(int groups) { return groups == 1 ? 8 * 32 * 68 * 4 : (size_t)groups * 4 * kUnitBytes; }
+static_assert(tiles_lds_bytes(1) >= 4 * kUnitBytes && tiles_lds_bytes(2) >= 4 * (66 * 64 + 32 * 68) * 4, "room for either");
 template <int kGroups, bool kRest>
 __global__ __launch_bounds__(kTileWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void attend_tiles_kernel(TileArgs a) {
     constexpr int kPair = 2 * kUnitBytes / 16;            // sixteen-byte pieces of two units
@@ -713,7 +754,6 @@ __global__ __launch_bounds__(kTileWaves * 64) __attribute__((amdgpu_waves_per_eu
 
     const int r = row_begin + min(wave * 32 + n, rows - 1), token = r / grp, head = hkv * grp + r - token * grp;
     const int sees = min(seq.kv - seq.n_new + token + 1, u_end * kUnitBlocks);
-    const size_t out_at = ((size_t)(seq.row0 + token) * a.Hq + head) * kGroup;
     half8_t q[8];
     {
         const uint4* from = reinterpret_cast<const uint4*>(a.q + (int64_t)(seq.row0 + token) * a.q_stride + head * kGroup) + h;
@@ -827,50 +867,83 @@ __global__ __launch_bounds__(kTileWaves * 64) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
         for (int i = 0; i < 64; ++i) o[i / 16][i % 16] = o[i / 16][i % 16] * mine + to[(2 + i) * 64] * theirs;
     }
-    // the lane holds dimensions 32 d + 8 (i / 4) + 4 h + i % 4 of its row
+    // The lane holds dimensions 32 d + 8 (i / 4) + 4 h + i % 4 of its row: 64 dimensions at a time the wavefront's rows pass through LDS, so that sixteen
+    // lanes store 64 neighbouring values.
     den += __shfl_xor(den, 32);
-    const int own = wave * 32 + n;
-    if (own >= rows) return;
-    if (a.splits > 1) {
-        const size_t part = (((size_t)at * a.Hkv + hkv) * a.tile_rows + own) * a.splits + split, all = (size_t)tiles * a.Hkv * a.tile_rows * a.splits;
-        float* to = a.lay.partial + part * kGroup + 4 * h;
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) *reinterpret_cast<float4_t*>(to + 32 * d + 8 * i) = float4_t{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
-        if (h == 0) {
-            a.lay.partial[all * kGroup + part * 2] = most * 0.08838834764831845f;
-            a.lay.partial[all * kGroup + part * 2 + 1] = den;
-        }
-        return;
+    const float scale = a.splits > 1 ? 1.0f : den > 0.0f ? 1.0f / den : 0.0f;
+    const size_t part = (((size_t)at * a.Hkv + hkv) * a.tile_rows + wave * 32) * a.splits + split, all = (size_t)tiles * a.Hkv * a.tile_rows * a.splits;
+    if (a.splits > 1 && h == 0 && wave * 32 + n < rows) {
+        float* ml = a.lay.partial + all * kGroup + (part + (size_t)n * a.splits) * 2;
+        ml[0] = most * 0.08838834764831845f;
+        ml[1] = den;
     }
-    const float one = den > 0.0f ? 1.0f / den : 0.0f;
+    constexpr int kTurnRow = 68;  // words of a row's 64 values
+    if constexpr (kGroups == 1) __syncthreads();  // the last units have been read
+    float* const turn = reinterpret_cast<float*>(smem) + (kGroups == 2 ? kTileWaves / 2 * 66 * 64 : 0) + wave * 32 * kTurnRow;
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+    for (int half = 0; half < 2; ++half) {
+        wave_lds_fence();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4_t v = float4_t{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]} * one;
-            const size_t to = out_at + 32 * d + 8 * i + 4 * h;
-            if (!kRest) {
+        for (int d = 0; d < 2; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float16_t& v = o[2 * half + d];
+                *reinterpret_cast<float4_t*>(turn + n * kTurnRow + 32 * d + 8 * i + 4 * h) = float4_t{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]} * scale;
+            }
+        wave_lds_fence();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = 4 * i + (lane >> 4), dim = 4 * (lane & 15);
+            const float4_t v = *reinterpret_cast<const float4_t*>(turn + row * kTurnRow + dim);
+            const int r = row_begin + wave * 32 + row, token = r / grp;
+            if (wave * 32 + row >= rows) continue;
+            const size_t to = ((size_t)(seq.row0 + token) * a.Hq + hkv * grp + r - token * grp) * kGroup + 64 * half + dim;
+            if (a.splits > 1) {
+                *reinterpret_cast<float4_t*>(a.lay.partial + (part + (size_t)row * a.splits) * kGroup + 64 * half + dim) = v;
+            } else if (kRest) {
+                *reinterpret_cast<float4_t*>(static_cast<float*>(a.out) + to) = v;
+            } else {
                 typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
                 *reinterpret_cast<half4_t*>(static_cast<_Float16*>(a.out) + to) = half4_t{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
-            } else {
-                *reinterpret_cast<float4_t*>(static_cast<float*>(a.out) + to) = v;
             }
         }
+    }
 }
 
-// merges the token ranges of a row: grid (tiles that there may be * Hkv, rows of a tile), 128 threads
-__global__ __launch_bounds__(kGroup) void attend_tiles_merge_kernel(TileArgs a) {
-    const int tiles = a.lay.tile_start[a.B], at = blockIdx.x / a.Hkv, hkv = blockIdx.x - at * a.Hkv, grp = a.Hq / a.Hkv;
+// merges the token ranges of rows: grid (tiles that there may be * Hkv, sets of 32 rows), 32 threads a row
+constexpr int kMergeThreads = 256, kMergeRows = 32;
+__global__ __launch_bounds__(kMergeThreads) void attend_tiles_merge_kernel(TileArgs a) {
+    const int tiles = a.lay.tile_start[a.B], at = blockIdx.x / a.Hkv, hkv = blockIdx.x - at * a.Hkv, grp = a.Hq / a.Hkv, n = a.splits;
     if (at >= tiles) return;
     const int b = place_of(a.lay.tile_start, a.B, at);
     const Sequence seq((args_t*)__builtin_amdgcn_kernarg_segment_ptr(), b);
-    const int r = (at - a.lay.tile_start[b]) * a.tile_rows + blockIdx.y, token = r / grp;
-    if (r >= seq.n_new * grp) return;
-    const size_t part = ((size_t)at * a.Hkv + hkv) * a.tile_rows * a.splits + (size_t)blockIdx.y * a.splits, all = (size_t)tiles * a.Hkv * a.tile_rows * a.splits;
-    const float v = merge_splits(a.lay.partial + all * kGroup + part * 2, a.lay.partial + part * kGroup + threadIdx.x, a.splits);
-    store_out((args_t*)__builtin_amdgcn_kernarg_segment_ptr(), ((size_t)(seq.row0 + token) * a.Hq + hkv * grp + r - token * grp) * kGroup + threadIdx.x, v);
+    const size_t first = ((size_t)at * a.Hkv + hkv) * a.tile_rows, all = (size_t)tiles * a.Hkv * a.tile_rows * n;
+    const int row_begin = (at - a.lay.tile_start[b]) * a.tile_rows, rows = min(a.tile_rows, seq.n_new * grp - row_begin), dim = 4 * (threadIdx.x & 31);
+#pragma unroll
+    for (int i = 0; i < kMergeRows * 32 / kMergeThreads; ++i) {
+        const int row = blockIdx.y * kMergeRows + i * (kMergeThreads / 32) + (threadIdx.x >> 5);
+        if (row >= rows) continue;
+        const float* ml = a.lay.partial + (all * kGroup) + (first + row) * n * 2;
+        const float* part = a.lay.partial + (first + row) * n * kGroup + dim;
+        float mx = -INFINITY, den = 0.0f;
+        for (int s = 0; s < n; ++s) mx = fmaxf(mx, ml[2 * s]);
+        float4_t num = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int s = 0; s < n; ++s) {
+            const float w = ml[2 * s] == -INFINITY ? 0.0f : __expf(ml[2 * s] - mx);
+            num += w * *reinterpret_cast<const float4_t*>(part + (size_t)s * kGroup);
+            den += w * ml[2 * s + 1];
+        }
+        num *= den > 0.0f ? 1.0f / den : 0.0f;
+        const int r = row_begin + row, token = r / grp;
+        const size_t to = ((size_t)(seq.row0 + token) * a.Hq + hkv * grp + r - token * grp) * kGroup + dim;
+        if (a.half) {
+            typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
+            *reinterpret_cast<half4_t*>(static_cast<_Float16*>(a.out) + to) = half4_t{(_Float16)num[0], (_Float16)num[1], (_Float16)num[2], (_Float16)num[3]};
+        } else {
+            *reinterpret_cast<float4_t*>(static_cast<float*>(a.out) + to) = num;
+        }
+    }
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------------
@@ -898,14 +971,17 @@ Plan plan_of(int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int6
     }
     p.bytes = p.few_bytes;
     if (wide) {
-#ifndef TMIN
-#define TMIN 2
-#endif
-        p.tile_rows = (long long)n_tokens * grp / 256 * Hkv >= TMIN * cus ? 256 : 128;
+        // A tile of 256 rows reads what it needs once for twice the rows, but there have to be enough of them: a 2048-token prompt, 32/8 heads, 69.3 us
+        // with 512 tiles of 128 rows, 78.1 us with 256 of 256; four chunks of up to 1024 tokens over 8192, 684 us with 980, 625 us with 490.
+        p.tile_rows = (long long)n_tokens * grp / 256 * Hkv * 2 >= 3ll * cus ? 256 : 128;
         const long long many = std::min<long long>(B, (long long)n_tokens * grp / ((long long)p.few + 1));  // sequences with more rows than `few`
-        p.wide_tiles = (int)((long long)n_tokens * grp / p.tile_rows + many);
+        const long long each = (rows + p.tile_rows - 1) / p.tile_rows;
+        p.wide_tiles = (int)(all ? each * B : std::min(each * many, (long long)n_tokens * grp / p.tile_rows + many));
         const long long units = std::min<long long>((std::min<long long>(total_kv, (long long)many * max_kv)) / kUnitBlocks + many, 0x7FFFFFFF);
         p.wide_units = (int)units;
+        // Split over the tokens where that makes a workgroup for every compute unit, and a range is worth its share of the merge: a chunk of 512 tokens
+        // over 4096, 128 tiles, 87.4 us whole, 71.7 us in two, 75.3 us in four; 64 tokens over 4096, 16 tiles, 99.1 us, in four 52.2 us, in eight
+        // 46.2 us; 1000 tokens over themselves, 128 tiles, 38.2 us, in two 40.1 us.
         const long long wgs = (long long)p.wide_tiles * Hkv;
         p.wide_splits = (int)std::min<long long>(std::min<long long>(std::max<long long>(1, cus / wgs), ((long long)max_kv + 511) / 512), 64);
         p.bytes += 2 * round_up(((size_t)B + 1) * 4) + round_up((size_t)units * 4) + (size_t)units * Hkv * kUnitBytes;
@@ -959,7 +1035,7 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
             at += round_up(bytes);
             return p;
         };
-        TileArgs t{args, {}, plan.tile_rows, plan.wide_splits};
+        TileArgs t{args, {}, plan.tile_rows, plan.wide_splits, B <= 64 && plan.wide_units < kLayoutMost && plan.wide_tiles < kLayoutMost};
         t.lay.unit_start = reinterpret_cast<int32_t*>(part(((size_t)B + 1) * 4));
         t.lay.tile_start = reinterpret_cast<int32_t*>(part(((size_t)B + 1) * 4));
         t.lay.seen = reinterpret_cast<uint32_t*>(part((size_t)plan.wide_units * 4));
@@ -967,8 +1043,10 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
         t.lay.partial = reinterpret_cast<float*>(at);
         t.lay.units = plan.wide_units;
         t.lay.tiles = plan.wide_tiles;
-        hipLaunchKernelGGL(attend_layout_kernel, dim3(1), dim3(64), 0, st, t);
-        ECCO_HIP_CHECK(hipGetLastError());
+        if (!t.layout) {
+            hipLaunchKernelGGL(attend_layout_kernel, dim3(1), dim3(64), 0, st, t);
+            ECCO_HIP_CHECK(hipGetLastError());
+        }
         const auto expand = [&](auto kernel) -> int {
             const size_t lds = expand_lds_bytes(std::max(mk->S, mv->S));
             const int rc = allow_lds(kernel, dev_id, lds);
@@ -993,7 +1071,7 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
         if (rc != ECCO_OK) return rc;
         ECCO_HIP_CHECK(hipGetLastError());
         if (plan.wide_splits > 1) {
-            hipLaunchKernelGGL(attend_tiles_merge_kernel, dim3((unsigned)plan.wide_tiles * Hkv, plan.tile_rows), dim3(kGroup), 0, st, t);
+            hipLaunchKernelGGL(attend_tiles_merge_kernel, dim3((unsigned)plan.wide_tiles * Hkv, plan.tile_rows / kMergeRows), dim3(kMergeThreads), 0, st, t);
             ECCO_HIP_CHECK(hipGetLastError());
         }
     }
