@@ -787,11 +787,12 @@ __global__ __launch_bounds__(kTileWaves * 64) __attribute__((amdgpu_waves_per_eu
         keep(0);
     }
     constexpr float kAhead = 8.0f;
+    float minus = -1.0f;
+    if constexpr (kRest) asm volatile("" : "+v"(minus));
     int which = 0;
     for (int u0 = u_begin; u0 < u_end; u0 += 2 * kGroups, which ^= 1) {
         const int u = u0 + 2 * group;  // (a group may have nothing left in the last round)
         const uint32_t there0 = seen0, there1 = seen1;
-        load(u + 2 * kGroups);
         __syncthreads();
         const half8_t* op = reinterpret_cast<const half8_t*>(lds + which * kPair) + lane;
         float16_t s[2];
@@ -807,6 +808,7 @@ __global__ __launch_bounds__(kTileWaves * 64) __attribute__((amdgpu_waves_per_eu
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
+        load(u + 2 * kGroups);
         if (u + 2 > whole || (__builtin_amdgcn_readfirstlane(there0) & __builtin_amdgcn_readfirstlane(there1)) != ~0u) {
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
@@ -830,14 +832,32 @@ __global__ __launch_bounds__(kTileWaves * 64) __attribute__((amdgpu_waves_per_eu
         }
         const float base = most == -INFINITY ? 0.0f : most * kScoreToExp2;
         half8_t p[4], rest[4];
+        const auto weight = [&](int i) { return __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], kScoreToExp2, -base)); };
+        if constexpr (kRest) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], kScoreToExp2, -base));
-            den += e;
-            const _Float16 e16 = (_Float16)e;
-            p[i / 8][i % 8] = e16;
-            if (kRest) rest[i / 8][i % 8] = (_Float16)(e - (float)e16);
+            for (int i = 0; i < 32; i += 2) {
+                typedef float float2_t __attribute__((ext_vector_type(2)));
+                const float2_t e = {weight(i), weight(i + 1)};
+                den += e[0];
+                den += e[1];
+                const half2_t rounded = __builtin_convertvector(e, half2_t);
+                // (the factor in a register: a product with a constant -1 becomes two conversions and a subtraction)
+                const half2_t left = __builtin_convertvector(float2_t{fmaf((float)rounded[0], minus, e[0]), fmaf((float)rounded[1], minus, e[1])}, half2_t);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    p[i / 8][i % 8 + j] = rounded[j];
+                    rest[i / 8][i % 8 + j] = left[j];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const float e = weight(i);
+                den += e;
+                p[i / 8][i % 8] = (_Float16)e;
+            }
         }
+        keep(which ^ 1);  // (here, and requested behind the first product: between the products they pass unnoticed)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -846,7 +866,6 @@ __global__ __launch_bounds__(kTileWaves * 64) __attribute__((amdgpu_waves_per_eu
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k], o[d], 0, 0, 0);
                 if (kRest) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, rest[k], o[d], 0, 0, 0);
             }
-        keep(which ^ 1);
     }
     if constexpr (kGroups == 2) {  // the second group's sums to the first
         float* const to = reinterpret_cast<float*>(smem) + wave * 66 * 64 + lane;
