@@ -73,6 +73,23 @@ def test_take(dev, B, page, most, new, spare, seed):
         assert np.array_equal(host(slots)[:-1], want[4]) and int(slots[-1]) == -99, n_tokens
 
 
+@pytest.mark.parametrize("B,page,most,new,spare", [(300, 16, 200, 60, 900), (1500, 16, 40, 9, 3000), (2, 1024, 9000, 30000, 80)])
+def test_take_with_a_count_of_its_own(dev, B, page, most, new, spare):
+    """Many rows: the same result whether the count is updated in place or written elsewhere, several times over."""
+    rng = np.random.default_rng(B)
+    held, table, free, count = _lists(rng, B, page, most, spare)
+    fresh = rng.integers(0, new + 1, B)
+    table = np.concatenate([table, np.full((B, -(-new // page)), -1)], 1)
+    n_tokens = int(fresh.sum())
+    want = R.take(held, fresh, table, free, count, page, n_tokens)
+    for i in range(4):
+        t, c, left = ints(table, dev), ints([count], dev), ints([-1], dev)
+        q_start, kv_len, slots = E.ecco_kv_pages_take(ints(held, dev), ints(fresh, dev), t, ints(free, dev), c, page, n_tokens, free_left=left if i % 2 else None)
+        assert int(left if i % 2 else c) == want[1] and (i % 2 == 0 or int(c) == count)
+        for got, w in zip((t, q_start, kv_len, slots), (want[0], *want[2:])):
+            assert np.array_equal(host(got), w)
+
+
 @pytest.mark.parametrize("count", [-3, 0, 5, 100])
 def test_take_reads_the_count_as_what_the_stack_can_hold(dev, count):
     held, fresh, table, free = [3, 0, 0], [20, 16, 16], np.full((3, 4), 0), np.arange(8)[::-1].copy()
@@ -274,6 +291,10 @@ ATTEND = [
     ("long", 8, 2, 16, [(70, 300)]),
     (64, 16, 2, 128, [(100, 20), (60, 59), (90, 0)]),                  # chunks of which much comes before position 0
     (16, 8, 1, 16, [(300, 1200)]),
+    (16, 4, 1, 16, [(1, 30 + 17 * i % 500) for i in range(100)]),      # ranges over more sequences than a wavefront has lanes
+    (16, 2, 1, 32, [(40 if i % 9 == 4 else 1 + i % 2, 60 + 31 * i % 200) for i in range(70)]),  # chunks among as many
+    (64, 128, 8, 64, [(790, 800)]),                                    # tiles of 256 rows
+    (16, 32, 4, 16, [(11, 3000), (2, 1100), (160, 2048)]),             # 8 rows per token: few, and tiles split over the tokens
 ]
 
 
@@ -321,6 +342,20 @@ def test_attend_lengths_beyond_the_bounds_touch_nothing_else(dev, oracle, models
         torch.cuda.synchronize()
         assert torch.isnan(guard[4:]).all()
         assert np.abs(host(guard[0]) - want[0]).max() <= 1e-3
+
+
+def test_attend_sequences_that_share_pages(dev, oracle, models):
+    """Two sequences with the same pages in front, and one that reads the same page twice."""
+    c = Cache(dev, oracle, models, 16, [150, 150, 64], 2, 32, 95)
+    c.table[1, :3] = c.table[0, :3]
+    c.table[2, 1] = c.table[2, 0]
+    for kept in (c.keys, c.values):
+        kept[1][:96] = kept[0][:96]
+        kept[2][32:] = kept[2][:32]
+    new, kv = [2, 60, 1], [150, 150, 64]
+    q = _queries(63, 8, 96)
+    want, bound = c.want(q, new, kv)
+    R.check_attend(c.run(dev, q, new, kv, False), want, bound, False)
 
 
 def test_attend_beyond_4_gib(dev, oracle, models):
@@ -456,6 +491,42 @@ def test_captured_step_replays(dev, oracle, models):
         assert torch.equal(out, want), i
         for x, y in ((a.table, b.table), (a.count, b.count), (a.lens, b.lens), (a.pool[1], b.pool[1]), (a.pool[2], b.pool[2])):
             assert torch.equal(x, y), i
+
+
+def test_captured_chunks_replay_with_other_lengths(dev, oracle, models):
+    """Chunks beside single tokens in a graph: the lengths, tables and queries of every replay are others, with eager work in between."""
+    Hq, Hkv, page, lens = 8, 2, 16, [700, 500, 260, 90]
+    c = Cache(dev, oracle, models, 16, lens, Hkv, page, 97)
+    n_tokens, max_new, max_kv, total = 200, 150, 700, 1600
+    q = torch.zeros((n_tokens, Hq, 128), dtype=torch.float16, device=dev)
+    starts, kv, out = ints(np.zeros(5), dev), ints(np.zeros(4), dev), torch.zeros((n_tokens, Hq, 128), dtype=torch.float32, device=dev)
+    ws = torch.empty((E.ecco_kv_attend_paged_workspace(n_tokens, 4, Hq, Hkv, max_new, max_kv, total),), dtype=torch.uint8, device=dev)
+    table = ints(c.table, dev)
+    call = lambda o, w: E.ecco_kv_attend_paged(*c.models, q, *c.pool, table, starts, kv, max_new, max_kv, total, w, o)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(out, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out, ws)
+    rng = np.random.default_rng(3)
+    for i in range(6):
+        new = [[150, 1, 1, 1], [1, 1, 1, 1], [1, 90, 0, 40], [0, 0, 100, 1], [5, 33, 130, 32], [1, 1, 3, 2]][i]
+        now = [int(rng.integers(max(n, 1), t + 1)) for n, t in zip(new, lens)]
+        qh = _queries(n_tokens, Hq, 700 + i)
+        q.copy_(torch.from_numpy(qh))
+        starts.copy_(ints(np.concatenate([[0], np.cumsum(new)]), dev))
+        kv.copy_(ints(now, dev))
+        out.fill_(-3.0)
+        graph.replay()
+        eager = call(torch.full_like(out, -3.0), None)
+        assert torch.equal(out, eager), i
+        rows = sum(new)
+        want, bound = c.want(qh[:rows], new, now)
+        R.check_attend(host(out)[:rows], want, bound, False, i)
+        assert bool((out[rows:] == -3.0).all())
 
 
 def test_streams_and_repeatability(dev, oracle, models):

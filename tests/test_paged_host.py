@@ -2,7 +2,8 @@
 of workspaces; and the plain definitions that the GPU tests compare with."""
 from __future__ import annotations
 
-import ctypes as C
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -124,3 +125,17 @@ def test_reference_attend():
     v = np.arange(256.0).reshape(2, 128)
     out, bound = R.attend(np.zeros((3, 128)), np.ones((2, 128)), v, np.array([[1, 0], [0, 0], [1, 1]], bool))
     assert np.array_equal(out[0], v[0]) and not out[1].any() and np.allclose(out[2], v.mean(0)) and (bound[1] == 0).all()
+
+
+@pytest.mark.skipif(not os.path.exists("/opt/rocm/llvm/bin/clang++"), reason="needs ROCm's clang++")
+def test_launch_plans_of_rows(tmp_path):
+    """tests/plans/rows_plans_main.cpp, compiled with the library's own header, walks the sizes that the kernel is launched with; undefined
+    arithmetic is trapped."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "rows_plans")
+    cmd = ["/opt/rocm/llvm/bin/clang++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I" + os.path.join(root, "include"),
+           "-I" + os.path.join(root, "paper_2505_06901_amd", "csrc"), os.path.join(root, "tests", "plans", "rows_plans_main.cpp"), "-o", exe]
+    build = subprocess.run(cmd, capture_output=True, text=True)
+    assert build.returncode == 0, build.stderr[-4000:]
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and "conditions hold" in run.stdout, (run.stdout[-2000:], run.stderr[-2000:])
