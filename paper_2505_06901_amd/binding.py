@@ -362,22 +362,23 @@ def _int32(t, n: int) -> int:
     return t.data_ptr()
 
 
-def _rows(x, n: int, heads: int) -> int:
-    """Device pointer of a CUDA FP16 tensor [n, heads, 128] whose rows are contiguous, at any distance from each other."""
+def _rows(x, n: int, heads: int):
+    """(device pointer, values from row to row) of a CUDA FP16 tensor [n, heads, 128] whose rows are contiguous, at any distance from each other."""
     assert x.dtype is (_types or _torch_types())[1] and x.is_cuda and x.shape == (n, heads, GROUP), "CUDA FP16 tensors [rows, heads, 128] expected"
-    stride = x.stride()
-    assert stride[2] == 1 and (stride[1] == GROUP or heads == 1), "a row's heads must be contiguous"
-    return x.data_ptr()
+    row, head, one = x.stride()
+    assert one == 1 and (head == GROUP or heads == 1), "a row's heads must be contiguous"
+    return x.data_ptr(), row if n > 1 else heads * GROUP
 
 
-def _row_stride(x, n: int, heads: int) -> int:
-    return x.stride(0) if n > 1 else heads * GROUP
-
-
-def _pool(blocks, meta, words: int):
-    """Device pointers of a pool's blocks and of its `words` meta words."""
-    assert blocks.is_cuda and blocks.is_contiguous() and blocks.numel() * blocks.element_size() == words * BLOCK_BYTES, "contiguous, 64 bytes per meta word"
-    return blocks.data_ptr(), _int32(meta, words)
+def _pool(k_blocks, k_meta, v_blocks, v_meta):
+    """(pages, heads, tokens of a page, the four device pointers) of a pool: blocks of 64 bytes, one per meta word [n_pages, heads, page_tokens]."""
+    shape = k_meta.shape
+    n_pages, heads, page_tokens = shape
+    size = n_pages * heads * page_tokens * BLOCK_BYTES
+    assert k_blocks.is_cuda and k_blocks.is_contiguous() and k_blocks.nbytes == size, "contiguous, 64 bytes per meta word"
+    assert v_blocks.is_cuda and v_blocks.is_contiguous() and v_blocks.nbytes == size, "contiguous, 64 bytes per meta word"
+    assert v_meta.shape == shape, "keys and values alike"
+    return n_pages, heads, page_tokens, k_blocks.data_ptr(), _int32(k_meta, 0), v_blocks.data_ptr(), _int32(v_meta, 0)
 
 
 def ecco_kv_pages_take(seq_len, new_len, page_table, free_pages, free_count, page_tokens: int, n_tokens: int, free_left=None, q_start=None,
@@ -409,10 +410,11 @@ def ecco_kv_pages_release(seq_len, keep_len, page_table, free_pages, free_count,
 
 
 def _append_paged(call, name: str, mk: Model, mv: Model, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots):
-    n_pages, H, page_tokens = k_meta.shape
-    n, words = k_new.shape[0], n_pages * H * page_tokens
-    _check(call(mk.handle, mv.handle, _rows(k_new, n, H), _rows(v_new, n, H), _row_stride(k_new, n, H), _row_stride(v_new, n, H),
-                *_pool(k_blocks, k_meta, words), *_pool(v_blocks, v_meta, words), _int32(slots, n), n, H, n_pages, page_tokens, _stream()), name)
+    n_pages, H, page_tokens, kb, km, vb, vm = _pool(k_blocks, k_meta, v_blocks, v_meta)
+    n = len(k_new)
+    k, k_stride = _rows(k_new, n, H)
+    v, v_stride = _rows(v_new, n, H)
+    _check(call(mk._h, mv._h, k, v, k_stride, v_stride, kb, km, vb, vm, _int32(slots, n), n, H, n_pages, page_tokens, _stream()), name)
 
 
 def ecco_kv_append_paged(mk: Model, mv: Model, k_new, v_new, k_blocks, k_meta, v_blocks, v_meta, slots):
@@ -435,10 +437,9 @@ def ecco_kv_attend_paged(mk: Model, mv: Model, q, k_blocks, k_meta, v_blocks, v_
     """q: CUDA FP16 [n_tokens, Hq, 128], a view into a wider tensor allowed; out: FP32 (the default) or FP16 [n_tokens, Hq, 128].  max_new,
     max_kv: at least the most new tokens and the most tokens of a sequence; total_kv: at least the tokens of all of them (default: B times
     max_kv); workspace: uint8 tensor of ecco_kv_attend_paged_workspace bytes."""
-    n_pages, Hkv, page_tokens = k_meta.shape
+    n_pages, Hkv, page_tokens, kb, km, vb, vm = _pool(k_blocks, k_meta, v_blocks, v_meta)
     B, max_pages = page_table.shape
     n_tokens, Hq, _ = q.shape
-    words = n_pages * Hkv * page_tokens
     if total_kv is None:
         total_kv = B * max_kv
     if out is None or workspace is None:
@@ -450,10 +451,10 @@ def ecco_kv_attend_paged(mk: Model, mv: Model, q, k_blocks, k_meta, v_blocks, v_
             workspace = torch.empty((size,), dtype=torch.uint8, device=q.device)
     half = out.dtype is (_types or _torch_types())[1]
     assert out.shape == q.shape and (half or out.dtype is _types[2]), "FP32 or FP16 outputs like q"
-    _check(lib().ecco_kv_attend_paged(mk.handle, mv.handle, _rows(q, n_tokens, Hq), _row_stride(q, n_tokens, Hq), *_pool(k_blocks, k_meta, words),
-                                      *_pool(v_blocks, v_meta, words), _int32(page_table, 0), _int32(q_start, B + 1), _int32(kv_len, B), n_tokens, B, Hq, Hkv,
-                                      n_pages, page_tokens, max_pages, max_new, max_kv, total_kv, _dp(workspace), workspace.numel() * workspace.element_size(),
-                                      _dp(out), int(half), _stream()), "ecco_kv_attend_paged")
+    ptr, stride = _rows(q, n_tokens, Hq)
+    _check(lib().ecco_kv_attend_paged(mk._h, mv._h, ptr, stride, kb, km, vb, vm, _int32(page_table, 0), _int32(q_start, B + 1), _int32(kv_len, B), n_tokens, B, Hq,
+                                      Hkv, n_pages, page_tokens, max_pages, max_new, max_kv, total_kv, _dp(workspace), workspace.nbytes, _dp(out), int(half),
+                                      _stream()), "ecco_kv_attend_paged")
     return out
 
 
