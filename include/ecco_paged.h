@@ -11,7 +11,8 @@
  *               Entries behind a sequence's last page may be anything.
  *   slot        page * page_tokens + token of the page.  n_pages * page_tokens and max_pages * page_tokens are at most 2^31 - 1.
  *   rows        the new tokens of a step, sequence by sequence: sequence b has the rows q_start[b] .. q_start[b + 1] - 1.
- * Contents of device memory are never trusted with an address: pages outside the pool are neither written nor read.
+ * Contents of device memory are never trusted with an address: pages outside the pool are neither written nor read.  Calls are launched on the
+ * calling thread's current device, which must hold the tensors (and, where there are models, the models).
  */
 #ifndef ECCO_PAGED_H
 #define ECCO_PAGED_H
@@ -34,6 +35,7 @@ extern "C" {
  * taken, no entry written, its slots -1, its kv_len 0 -- if not all of its rows lie below n_tokens, if it needs more than max_pages, or
  * if the pages that it and the sequences before it need are more than there are (one that needs none is served all the same).
  * Otherwise kv_len = seq_len + new_len.  q_start is the running sum of new_len, at most n_tokens; rows from q_start[B] on get slot -1.
+ * Apart from free_left, outputs must not overlap inputs: lengths are advanced by a copy of kv_len behind the step.
  * Errors: EINVAL (null), ESHAPE (B, max_pages, n_pages <= 0, n_tokens < 0, page_tokens, sizes over 2^31 - 1), EALIGN (4 bytes), EHIP.
  * With n_tokens == 0 slots may be null. */
 int ecco_kv_pages_take(const int32_t* seq_len, const int32_t* new_len, int B, int page_tokens, int max_pages, int32_t* page_table,
@@ -72,9 +74,10 @@ int ecco_kv_append_paged_minmax(const ecco_model* mk, const ecco_model* mv, cons
  *              unwritten or see too little; nothing out of range is touched.
  *   workspace  device, 256-byte aligned, workspace_bytes >= ecco_kv_attend_paged_workspace(...) of the same sizes on the models' device,
  *              contents irrelevant before and after.  Calls that share one must not overlap; null if 0 bytes are asked for.
- * Sequences with few rows per key/value head are decoded once per 16 rows, on the way into the products; those with more are decoded into the
- * workspace, as operands of the matrix cores, and then read by all their rows.  The softmax's sums are FP32; probabilities enter the second
- * product as two FP16 numbers (22 bits) where out is FP32, as one where it is FP16 and the sequence has many rows.
+ * Sequences with few rows per key/value head (n * Hq / Hkv up to 32; beside longer ones, a token) are decoded on the way into the products; those with
+ * more are decoded into the workspace, as operands of the matrix cores, and then read by all their rows.  The softmax's sums are FP32; probabilities
+ * enter the second product as two FP16 numbers (22 bits) where out is FP32, as one where it is FP16 and the sequence has many rows.  The
+ * same call gives the same bits; other bounds may cut the sums elsewhere.
  * A block with a scale that is not finite (never written by the encoder) makes all rows of its sequence unspecified.
  * Errors: EINVAL (also a workspace too small), ESHAPE, EALIGN, EHIP.  n_tokens == 0 is a no-op. */
 size_t ecco_kv_attend_paged_workspace(int device, int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv);

@@ -1,4 +1,9 @@
 // Attention of a step's new tokens over the paged compressed cache (include/ecco_paged.h).
+//
+// What bounds it.  With few rows (new tokens times query heads that share a key/value head) a block's 128 values are decoded for a handful of products:
+// the decoders' table reads from LDS are the limit, about 22 blocks per ns on the whole chip, and a chain of 64 values, 4 us, where there are few
+// blocks.  They are decoded on the way into the products then (attend_rows_kernel).  With many rows it is the matrix cores: sequences are decoded once,
+// into operands in the workspace (attend_expand_kernel, 9 blocks per ns with the writing), and the products run from there (attend_tiles_kernel).
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 
@@ -86,8 +91,8 @@ __device__ __forceinline__ UnitPages unit_pages(int b, int t0, int last) {
     p.page[1] = row[(min(t0 + kUnitBlocks / 2, last) >> a->shift) + zero];
     return p;
 }
-// As load_unit of the contiguous caches: the payload pieces of this lane and the meta word of the unit's block `tok`, which it decodes.  Slots of a page are all readable, whether they hold a token or not; of a page that is none the first one's are read.
-// ok: whether the page of token `tok` is one
+// As load_unit of the contiguous caches: the payload pieces of this lane and the meta word of the unit's block `tok`, which it decodes.  Slots of a
+// page are all readable, whether they hold a token or not; of a page that is none the first one's are read.  ok: whether the page of token `tok` is one
 template <bool kValues>
 __device__ __forceinline__ UnitLoad load_unit(const UnitPages& p, int hkv, int t0, int lane, int tok, bool& ok) {
     args_t* a = fresh_args();
@@ -115,16 +120,17 @@ __device__ __forceinline__ UnitLoad load_unit(const UnitPages& p, int hkv, int t
 // scores come from v_mfma_f32_32x32x16_f16 instead: one product per eight values and chain for 32 tokens and up to 32 rows, no half of its operand
 // zeroed, eight query values of one row per lane (lane l decodes chain l / 32 of token l % 32).  With 32 rows the second product runs over two tiles
 // of 16.
+//
 // grid: ranges of the tokens (Range) that there may be, times Hkv.  Where a sequence has several, the workspace takes 128 outputs of each range
 // and row, then (maximum, denominator) pairs, and a second kernel merges them.
+// Five new tokens each of eight sequences of 570 to 2880 tokens, 32/8 heads: 48.6 us with 16 rows at a time, every block decoded twice; 30.7 us so.
+
 // Which range of which sequence a workgroup takes.  Ranges are of one length for all sequences, so that one long sequence beside short ones
 // gets many of them: the least length, kRangeLeast units or more, with which all workgroups find a place at once, looked for among 64 (one per
 // lane).  Every wavefront works it out for itself from all the sequences' lengths, a load for up to 64 of them.  (Eight sequences of 690 to
 // 3398 tokens, 8 x 4 heads: 29.3 us with four ranges each, 27.0 us with a workgroup per compute unit, 24.8 us with two; 16 sequences up to 4096 tokens
 // 56.8 us and 50.6 us.)  A merge costs 3 to 4 us, as much as six units more per range: ranges of 4 and 12 units at the least, one sequence of 1000
 // tokens 15.7 and 21.2 us, of 8 units 16.5 us; four of 2000 20.0, 21.6 and 17.1 us.
-constexpr int kRangeLeast = 8;        // units: one for each wavefront
-constexpr int kRangeSequences = 256;  // sequences up to which ranges are cut
 struct Range {
     int b, hkv;          // sequence, key/value head; b < 0: nothing to do
     int first, n, index; // ranges of the sequences before this one, of this one, and which of its it is
@@ -164,8 +170,7 @@ __device__ __forceinline__ Range find_range(args_t* a, int lane) {
         if (c * 64 + lane < B && rows > 0 && rows <= a->few) units[c] = of[c].kv > 0 ? units_of(of[c].kv) : 0;
         total += max(units[c], 0);
     }
-    total = __builtin_amdgcn_readlane(wave_scan(total, lane), 63);
-    const int least = max(kRangeLeast, (int)ceilf((float)total * (float)Hkv / (float)a->cus * 0.9999f)), step = max(1, least / 16);
+    const int least = range_least(wave_sum((float)total), Hkv, a->cus), step = max(1, least / 16);
     int length = least + least / 4;
     if (B <= 32) {
         const int mine = least + lane * step;
@@ -523,6 +528,7 @@ __global__ __launch_bounds__(kGroup) void attend_rows_merge_kernel(PagedArgs arg
     const Sequence seq(a, b);
     const int r = blockIdx.y, token = r / grp;
     if (r >= seq.n_new * grp || seq.n_new * grp > args.few || ranges.y == 1) return;
+    if (ranges.x < 0 || ranges.y < 1 || ((int64_t)ranges.x + ranges.y) * args.Hkv > n_wgs) return;  // not in the workspace
     const size_t at = ((size_t)ranges.x * args.Hkv + (size_t)hkv * ranges.y) * kernel_rows + (size_t)r * ranges.y, total = (size_t)n_wgs * kernel_rows;
     const float v = merge_splits(args.ws + total * kGroup + at * 2, args.ws + at * kGroup + threadIdx.x, ranges.y);
     store_out(a, ((size_t)(seq.row0 + token) * a->Hq + hkv * grp + r - token * grp) * kGroup + threadIdx.x, v);
@@ -530,7 +536,8 @@ __global__ __launch_bounds__(kGroup) void attend_rows_merge_kernel(PagedArgs arg
 
 // ---- many rows per key/value head ----------------------------------------------------------------------------------------
 // Decoding a block costs as much as the products of its 128 values with a few hundred rows, so a sequence with more than kFewRows rows per
-// key/value head is decoded once, into the workspace, and then read by all its rows.  What is written are the operands of
+// key/value head (beside such ones, with more rows than a token has) is decoded once, into the workspace, and then read by all its rows.  What is
+// written are the operands of
 // v_mfma_f32_32x32x16_f16 in the order in which its lanes take them, a unit of 32 tokens at a time (16 KB):
 //   K   A operands of S[token][row] = sum_dim K[token][dim] q[row][dim]: eight of 1 KB, the s-th for dimensions 16 s .. + 15; lane l takes token
 //       l % 32 and the eight dimensions from 16 s + 8 (l / 32) on
@@ -555,7 +562,6 @@ struct TileArgs : PagedArgs {
     int tile_rows, splits;
     int layout;  // whether attend_expand_kernel finds the layout by itself
 };
-typedef const __attribute__((address_space(4))) TileArgs tile_args_t;
 
 // What sequence 64 c + l of a batch takes, for lane l: units of 32 tokens in the workspace, tiles of rows.  Nothing if it has few rows.
 struct Takes {
@@ -629,7 +635,9 @@ __device__ __forceinline__ int place_of(const int32_t* start, int B, int v) {
     return lo;
 }
 
-// Decodes units into operands: grid (workgroups, 2), keys and values.  Lane l decodes chain l / 32 of token l % 32.
+// Decodes units into operands: grid (workgroups, 2), keys and values.  Lane l decodes chain l / 32 of token l % 32; eight decoded key values are sixteen
+// bytes of an operand as they are, values pass through a tile of 16 dimensions in LDS, where tokens become neighbours.  8192 tokens, 8 heads, 64
+// patterns: 14.7 us, 8.9 blocks per ns; 33.5 MB are written.
 constexpr int kExpandWaves = 16;
 constexpr int kTurnStride = 20;  // words per dimension of the tile in which values are turned
 constexpr size_t expand_lds_bytes(int S) { return (table_words(S) + (size_t)kExpandWaves * (kUnitWords + 16 * kTurnStride)) * 4; }
@@ -714,7 +722,16 @@ __global__ __launch_bounds__(kExpandWaves * 64) void attend_expand_kernel(TileAr
     else expand<kLongV, true>(a);
 }
 
-// The products: a workgroup takes a tile of rows of one sequence and key/value head, a wavefront 32 kCols of them, over a range of the sequence's tokens.
+// The products: a workgroup takes a tile of rows of one sequence and key/value head, a wavefront 32 of them, over a range of the sequence's tokens, two
+// units at a time.  The scores of a pair of units, 32 per lane and all of one row, become probabilities and the next product's operand where they are;
+// they are relative to `most`, which follows a row's largest score only when that is ahead by more than 2^kAhead, so that probabilities stay far within
+// FP16's range and the sums are rescaled a few times per row instead of once per pair.  For FP32 outputs what an FP16 probability leaves of the
+// FP32 one goes through a product of its own (the error against 64 bits 1.1e-6 in a step of two 450-token chunks over 4096); for FP16 outputs it is left out: half a step of a probability,
+// at random, adds 30 % to the error that the outputs' own rounding makes (2.7e-4 for 2.1e-4).
+// What bounds it: a 4096-token chunk over 8192, 32/8 heads, FP16 outputs, 397 us for 412 GFLOP; in a run of 422 us the matrix cores were busy 54 % of
+// the time at 1.87 GHz.  Power holds the clock there: with zeros for queries and values the whole call took 347 us beside 439, and the library's
+// product of 8192^3 reaches 1.16 PFLOP/s with random values and 1.72 with zeros.  Two wavefronts of a SIMD held in opposite phases by barriers:
+// 501 us beside 422; exponentials left out, for the measurement alone: the call 401 us beside 433.
 constexpr float kScoreToExp2 = 0.08838834764831845f * 1.4426950408889634f;  // log2(e) / sqrt(128)
 
 // the larger of the two lanes' values that hold a row's scores, l and l + 32
@@ -1071,7 +1088,7 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
             const int rc = allow_lds(kernel, dev_id, lds);
             if (rc != ECCO_OK) return rc;
             const long long wgs = ((long long)plan.wide_units * Hkv + kExpandWaves - 1) / kExpandWaves;
-            hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<long long>(wgs, cus / 2), 2), dim3(kExpandWaves * 64), lds, st, t);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)std::max<long long>(1, std::min<long long>(wgs, cus / 2)), 2), dim3(kExpandWaves * 64), lds, st, t);
             ECCO_HIP_CHECK(hipGetLastError());
             return ECCO_OK;
         };

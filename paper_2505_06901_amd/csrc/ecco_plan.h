@@ -19,6 +19,17 @@ constexpr int decode_table_words(int S, bool lng) { return S * (kPeekEntries + k
 // Units of 32 tokens in a capacity of `tokens`, which may be any positive number up to 2^31 - 1: of that many units, the tokens no longer
 // fit an int.
 constexpr int units_of(int tokens) { return (tokens - 1) / kUnitBlocks + 1; }
+// Ranges of a step over pages: sequences are cut into ranges of one length, so that those of all heads find a place at once among `places`
+// workgroups.  The least length for `total` units of all sequences.  The total is FP32, since it may exceed an int; ranges of this length or
+// more, and at least one per sequence, are at most places / Hkv and one per sequence.
+constexpr int kRangeLeast = 8;        // units: one for each wavefront
+constexpr int kRangeSequences = 256;  // sequences up to which ranges are cut
+constexpr int range_least(float total, int Hkv, int places) {
+    const float share = total * (float)Hkv / (float)places * 0.9999f;
+    if (share >= 134217728.0f) return 134217728;  // longer than any sequence
+    const int whole = (int)share;
+    return std::max(kRangeLeast, whole + ((float)whole < share ? 1 : 0));
+}
 // Tokens of `units` units, or more than a span ever holds
 constexpr int kSpanMax = 8192, kSpanLeast = 2048;
 constexpr int span_tokens(int units) { return std::min(units, kSpanMax / kUnitBlocks + 1) * kUnitBlocks; }

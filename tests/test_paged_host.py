@@ -139,3 +139,15 @@ def test_launch_plans_of_rows(tmp_path):
     assert build.returncode == 0, build.stderr[-4000:]
     run = subprocess.run([exe], capture_output=True, text=True, timeout=300)
     assert run.returncode == 0 and "conditions hold" in run.stdout, (run.stdout[-2000:], run.stderr[-2000:])
+
+
+def test_ranges_fit_what_the_launch_holds(tmp_path):
+    """tests/plans/range_plans_main.cpp: sequences so long that their units together exceed an int included; undefined arithmetic is trapped."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "range_plans")
+    cmd = ["/opt/rocm/llvm/bin/clang++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I" + os.path.join(root, "include"),
+           "-I" + os.path.join(root, "paper_2505_06901_amd", "csrc"), os.path.join(root, "tests", "plans", "range_plans_main.cpp"), "-o", exe]
+    build = subprocess.run(cmd, capture_output=True, text=True)
+    assert build.returncode == 0, build.stderr[-4000:]
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and "conditions hold" in run.stdout, (run.stdout[-2000:], run.stderr[-2000:])
