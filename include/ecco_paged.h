@@ -35,9 +35,9 @@ extern "C" {
  * taken, no entry written, its slots -1, its kv_len 0 -- if not all of its rows lie below n_tokens, if it needs more than max_pages, or
  * if the pages that it and the sequences before it need are more than there are (one that needs none is served all the same).
  * Otherwise kv_len = seq_len + new_len.  q_start is the running sum of new_len, at most n_tokens; rows from q_start[B] on get slot -1.
- * Apart from free_left, outputs must not overlap inputs: lengths are advanced by a copy of kv_len behind the step.
- * Errors: EINVAL (null), ESHAPE (B, max_pages, n_pages <= 0, n_tokens < 0, page_tokens, sizes over 2^31 - 1), EALIGN (4 bytes), EHIP.
- * With n_tokens == 0 slots may be null. */
+ * Apart from free_left, which may be free_count, outputs must not overlap inputs: lengths are advanced by a copy of kv_len behind the step.
+ * Errors: EINVAL (null), ESHAPE (B, max_pages, n_pages <= 0, n_tokens < 0, page_tokens, sizes over 2^31 - 1), EALIGN (4 bytes), EINVAL (kv_len is
+ * seq_len or new_len), EHIP.  With n_tokens == 0 slots may be null. */
 int ecco_kv_pages_take(const int32_t* seq_len, const int32_t* new_len, int B, int page_tokens, int max_pages, int32_t* page_table,
                        const int32_t* free_pages, const int32_t* free_count, int32_t* free_left, int n_pages,
                        int n_tokens, int32_t* q_start, int32_t* kv_len, int32_t* slots, void* stream);

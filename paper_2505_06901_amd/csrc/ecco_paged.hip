@@ -637,7 +637,7 @@ __device__ __forceinline__ int place_of(const int32_t* start, int B, int v) {
 
 // Decodes units into operands: grid (workgroups, 2), keys and values.  Lane l decodes chain l / 32 of token l % 32; eight decoded key values are sixteen
 // bytes of an operand as they are, values pass through a tile of 16 dimensions in LDS, where tokens become neighbours.  8192 tokens, 8 heads, 64
-// patterns: 14.7 us, 8.9 blocks per ns; 33.5 MB are written.
+// patterns: 14.7 to 15.6 us, 8.4 to 8.9 blocks per ns; 33.5 MB are written.
 constexpr int kExpandWaves = 16;
 constexpr int kTurnStride = 20;  // words per dimension of the tile in which values are turned
 constexpr size_t expand_lds_bytes(int S) { return (table_words(S) + (size_t)kExpandWaves * (kUnitWords + 16 * kTurnStride)) * 4; }
@@ -728,7 +728,7 @@ __global__ __launch_bounds__(kExpandWaves * 64) void attend_expand_kernel(TileAr
 // FP16's range and the sums are rescaled a few times per row instead of once per pair.  For FP32 outputs what an FP16 probability leaves of the
 // FP32 one goes through a product of its own (the error against 64 bits 1.1e-6 in a step of two 450-token chunks over 4096); for FP16 outputs it is left out: half a step of a probability,
 // at random, adds 30 % to the error that the outputs' own rounding makes (2.7e-4 for 2.1e-4).
-// What bounds it: a 4096-token chunk over 8192, 32/8 heads, FP16 outputs, 397 us for 412 GFLOP; in a run of 422 us the matrix cores were busy 54 % of
+// What bounds it: a 4096-token chunk over 8192, 32/8 heads, FP16 outputs, 397 to 403 us for 412 GFLOP; in a run of 422 us the matrix cores were busy 54 % of
 // the time at 1.87 GHz.  Power holds the clock there: with zeros for queries and values the whole call took 347 us beside 439, and the library's
 // product of 8192^3 reaches 1.16 PFLOP/s with random values and 1.72 with zeros.  Two wavefronts of a SIMD held in opposite phases by barriers:
 // 501 us beside 422; exponentials left out, for the measurement alone: the call 401 us beside 433.

@@ -263,6 +263,7 @@ int ecco_kv_pages_take(const int32_t* seq_len, const int32_t* new_len, int B, in
     for (const void* p : {(const void*)seq_len, (const void*)new_len, (const void*)page_table, (const void*)free_pages, (const void*)free_count, (const void*)free_left,
                           (const void*)q_start, (const void*)kv_len, (const void*)slots})
         if (!aligned(p, 4)) return ECCO_EALIGN;
+    if (kv_len == seq_len || kv_len == new_len) return ECCO_EINVAL;  // one workgroup writes what others may yet have to read
     TakeArgs a{seq_len, new_len, page_table, free_pages, free_count, free_left, q_start, kv_len, slots, B, shift_of(page_tokens), max_pages, n_pages, n_tokens};
     hipStream_t st = static_cast<hipStream_t>(stream);
     // few sequences and rows: a workgroup whose barriers meet four wavefronts and not sixteen

@@ -151,3 +151,13 @@ def test_ranges_fit_what_the_launch_holds(tmp_path):
     assert build.returncode == 0, build.stderr[-4000:]
     run = subprocess.run([exe], capture_output=True, text=True, timeout=300)
     assert run.returncode == 0 and "conditions hold" in run.stdout, (run.stdout[-2000:], run.stderr[-2000:])
+
+
+@pytest.mark.parametrize("other", ["seq_len", "new_len"])
+def test_lengths_are_not_advanced_in_place(other):
+    """kv_len is written by one workgroup while others read the lengths, so it cannot be one of them: refused behind all other checks."""
+    apart = {k: FAKE + 0x100 * i for i, k in enumerate(TAKE) if TAKE[k] == FAKE}
+    same = {**apart, "kv_len": apart[other]}
+    assert _call("ecco_kv_pages_take", TAKE, **same) == EINVAL
+    assert _call("ecco_kv_pages_take", TAKE, **{**same, "B": 0}) == ESHAPE
+    assert _call("ecco_kv_pages_take", TAKE, **{**same, "slots": ODD2}) == EALIGN
