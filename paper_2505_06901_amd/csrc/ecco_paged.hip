@@ -125,6 +125,9 @@ __device__ __forceinline__ UnitLoad load_unit(const UnitPages& p, int hkv, int t
 // and row, then (maximum, denominator) pairs, and a second kernel merges them.
 // Five new tokens each of eight sequences of 570 to 2880 tokens, 32/8 heads: 48.6 us with 16 rows at a time, every block decoded twice; 30.7 us so.
 
+constexpr float kLog2E = 1.4426950408889634f;
+constexpr float kWeightTop = 15.0f;  // the largest weight's power of two: FP16 holds up to 2^16; numerators and denominators share it
+
 // Which range of which sequence a workgroup takes.  Ranges are of one length for all sequences, so that one long sequence beside short ones
 // gets many of them: the least length, kRangeLeast units or more, with which all workgroups find a place at once, looked for among 64 (one per
 // lane).  Every wavefront works it out for itself from all the sequences' lengths, a load for up to 64 of them.  (Eight sequences of 690 to
@@ -407,8 +410,10 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
             const Lane L = lane_setup(TV, mw, Sv);
             const _Float16 sh16 = __builtin_bit_cast(_Float16, (unsigned short)(mw & 0xFFFFu));
             const half2_t s2 = {sh16, sh16};
-            // B operand: probabilities of row l % 16 of the tile for tokens 8 * (l / 16) .. + 7 of the unit, 0 for what is not seen.  What an
-            // FP16 probability leaves of the FP32 one is the operand of a product of its own, or with up to eight rows of columns 8..15.
+            // B operand: weights of row l % 16 of the tile for tokens 8 * (l / 16) .. + 7 of the unit, 0 for what is not seen.  What an FP16 weight
+            // leaves of the FP32 one is the operand of a product of its own, or with up to eight rows of columns 8..15.  The largest weight is
+            // 2^kWeightTop, so that the pair keeps 22 bits down to 2^-18 of it and is off by 2^-40 of it at the most below (2^-25 with weights up to 1:
+            // the many tokens far behind a leading one vanished from the sum, but not from the denominator).
             const float taken = !kWide && n < 8 ? 0.0f : 1.0f;
             half8_t pb[kTiles], rest[kTiles];
 #pragma unroll
@@ -417,7 +422,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
                 const float4_t s[2] = {reinterpret_cast<const float4_t*>(score)[0], reinterpret_cast<const float4_t*>(score)[1]};
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float p = 16 * t + row < rows ? __expf(s[i >> 2][i & 3] - base[t]) : 0.0f;
+                    const float p = 16 * t + row < rows ? __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3] - base[t], kLog2E, kWeightTop)) : 0.0f;
                     pb[t][i] = (_Float16)p;
                     rest[t][i] = (_Float16)fmaf(-taken, (float)pb[t][i], p);
                     run_den[t] += p;
