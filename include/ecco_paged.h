@@ -75,8 +75,9 @@ int ecco_kv_append_paged_minmax(const ecco_model* mk, const ecco_model* mv, cons
  *   workspace  device, 256-byte aligned, workspace_bytes >= ecco_kv_attend_paged_workspace(...) of the same sizes on the models' device,
  *              contents irrelevant before and after.  Calls that share one must not overlap; null if 0 bytes are asked for.
  * Sequences with few rows per key/value head (n * Hq / Hkv up to 32; beside longer ones, a token) are decoded on the way into the products; those with
- * more are decoded into the workspace, as operands of the matrix cores, and then read by all their rows.  The softmax's sums are FP32; probabilities
- * enter the second product as two FP16 numbers (22 bits) where out is FP32, as one where it is FP16 and the sequence has many rows.  The
+ * more are decoded into the workspace, as operands of the matrix cores, and then read by all their rows.  The softmax's sums are FP32; its weights
+ * enter the second product as two FP16 numbers (22 bits), or as one (11 bits) where out is FP16 and the sequence has many rows.  They are scaled so that
+ * the largest is at FP16's top: whatever its size, a weight is off by 2^-40 of the largest at the most (few rows) or 2^-36 (many), or by its last bit.  The
  * same call gives the same bits; other bounds may cut the sums elsewhere.
  * A block with a scale that is not finite (never written by the encoder) makes all rows of its sequence unspecified.
  * Errors: EINVAL (also a workspace too small), ESHAPE, EALIGN, EHIP.  n_tokens == 0 is a no-op. */

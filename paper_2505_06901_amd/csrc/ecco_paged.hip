@@ -729,10 +729,14 @@ __global__ __launch_bounds__(kExpandWaves * 64) void attend_expand_kernel(TileAr
 
 // The products: a workgroup takes a tile of rows of one sequence and key/value head, a wavefront 32 of them, over a range of the sequence's tokens, two
 // units at a time.  The scores of a pair of units, 32 per lane and all of one row, become probabilities and the next product's operand where they are;
-// they are relative to `most`, which follows a row's largest score only when that is ahead by more than 2^kAhead, so that probabilities stay far within
-// FP16's range and the sums are rescaled a few times per row instead of once per pair.  For FP32 outputs what an FP16 probability leaves of the
-// FP32 one goes through a product of its own (the error against 64 bits 1.1e-6 in a step of two 450-token chunks over 4096); for FP16 outputs it is left out: half a step of a probability,
-// at random, adds 30 % to the error that the outputs' own rounding makes (2.7e-4 for 2.1e-4).
+// they are relative to `most`, which follows a row's largest score only when that is ahead by more than 2^kAhead, so that the sums are rescaled a
+// few times per row instead of once per pair, and the score `most` has the weight 2^(kWeightTop - kAhead), so that weights reach FP16's top and the
+// smallest ones keep their bits: the second number of a pair, or the first one alone, is whole down to 2^-25 of that weight and off by 2^-36 of it at
+// the most below.  (kAhead 8, 4, 2, 0: a 4096-token chunk over 8192 416.9, 421.4, 425.2, 431.7 us; 414.8 with 8 and the weight 1, which lost
+// the tokens far behind a leading one.)  For FP32 outputs what an FP16 probability leaves of the
+// FP32 one goes through a product of its own (the error against 64 bits 1.1e-6 in a step of two 450-token chunks over 4096); for FP16 outputs it is left out: half a step of a
+// weight, at random, adds 19 % to the error that the outputs' own rounding makes (2.5e-4 for 2.1e-4), and without it the chunk above takes 441 us
+// instead of 572.
 // What bounds it: a 4096-token chunk over 8192, 32/8 heads, FP16 outputs, 397 to 403 us for 412 GFLOP; in a run of 422 us the matrix cores were busy 54 % of
 // the time at 1.87 GHz.  Power holds the clock there: with zeros for queries and values the whole call took 347 us beside 439, and the library's
 // product of 8192^3 reaches 1.16 PFLOP/s with random values and 1.72 with zeros.  Two wavefronts of a SIMD held in opposite phases by barriers:
@@ -808,7 +812,7 @@ __global__ __launch_bounds__(kTileWaves * 64) __attribute__((amdgpu_waves_per_eu
         load(u_begin + 2 * group);
         keep(0);
     }
-    constexpr float kAhead = 8.0f;
+    constexpr float kAhead = 4.0f;
     float minus = -1.0f;
     if constexpr (kRest) asm volatile("" : "+v"(minus));
     int which = 0;
@@ -852,7 +856,7 @@ __global__ __launch_bounds__(kTileWaves * 64) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
             for (int d = 0; d < 4; ++d) o[d] *= alpha;
         }
-        const float base = most == -INFINITY ? 0.0f : most * kScoreToExp2;
+        const float base = most == -INFINITY ? 0.0f : fmaf(most, kScoreToExp2, kAhead - kWeightTop);
         half8_t p[4], rest[4];
         const auto weight = [&](int i) { return __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], kScoreToExp2, -base)); };
         if constexpr (kRest) {

@@ -89,6 +89,12 @@ def test_small_weights_few_rows(dev, oracle, models, case, half):
 
 
 @pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("case", range(5, 8))
+def test_small_weights_many_rows(dev, oracle, models, case, half):
+    _check(dev, oracle, models, case, half, LEADS, 200 + case)
+
+
+@pytest.mark.parametrize("half", [False, True])
 @pytest.mark.parametrize("case", [0, 5])
 def test_a_lead_that_comes_late(dev, oracle, models, case, half):
     """The other way round: leads below zero put the first token behind all others, so that it does not weigh at all and the rest is a mean."""
