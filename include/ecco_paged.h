@@ -79,6 +79,7 @@ int ecco_kv_append_paged_minmax(const ecco_model* mk, const ecco_model* mv, cons
  * enter the second product as two FP16 numbers (22 bits), or as one (11 bits) where out is FP16 and the sequence has many rows.  They are scaled so that
  * the largest is at FP16's top: whatever its size, a weight is off by 2^-40 of the largest at the most (few rows) or 2^-36 (many), or by its last bit.  The
  * same call gives the same bits; other bounds may cut the sums elsewhere.
+ * A query that is not finite makes its own outputs NaN, and no others.
  * A block with a scale that is not finite (never written by the encoder) makes all rows of its sequence unspecified.
  * Errors: EINVAL (also a workspace too small), ESHAPE, EALIGN, EHIP.  n_tokens == 0 is a no-op. */
 size_t ecco_kv_attend_paged_workspace(int device, int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv);

@@ -340,7 +340,10 @@ __device__ __forceinline__ void store_unit(uint32_t* wbuf, const UnitLoad& u, in
 
 // The merge of n_splits partial results of one query head, a dimension per thread: ml holds their (maximum, denominator) pairs, part this
 // dimension's unnormalised outputs, kGroup apart.
-__device__ __forceinline__ float merge_splits(const float* __restrict__ ml, const float* __restrict__ part, int n_splits) {
+struct Merged {
+    float num, den;
+};
+__device__ __forceinline__ Merged merge_splits(const float* __restrict__ ml, const float* __restrict__ part, int n_splits) {
     // Sixteen splits at a time (four or eight where there are no more) with all their loads in flight together, indices
     // clamped; the additions run in split order.  An empty split (maximum -inf, zeros) gets weight 0, also when every
     // split is empty (mx = -inf).  The kernel is bound by the latency of the partial results, which come from memory: up to
@@ -381,7 +384,7 @@ __device__ __forceinline__ float merge_splits(const float* __restrict__ ml, cons
         mx = wave_all(mx, [](float a, float b) { return fmaxf(a, b); });
         for (int s0 = 0; s0 < n_splits; s0 += 16) batch(std::integral_constant<int, 16>{}, s0, mx);
     }
-    return den > 0.0f ? num / den : 0.0f;
+    return {num, den};
 }
 
 }  // namespace ecco_chain

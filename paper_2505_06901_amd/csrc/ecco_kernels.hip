@@ -973,7 +973,8 @@ __global__ __launch_bounds__(kGroup) void kv_attend_combine_kernel(const float* 
     const size_t bh = blockIdx.x;
     const float* ml = ws + (size_t)n_heads * n_splits * kGroup + bh * n_splits * 2;
     const float* part = ws + bh * n_splits * kGroup + threadIdx.x;
-    out[bh * kGroup + threadIdx.x] = merge_splits(ml, part, n_splits);
+    const Merged v = merge_splits(ml, part, n_splits);
+    out[bh * kGroup + threadIdx.x] = v.den > 0.0f ? v.num / v.den : 0.0f;
 }
 
 // ---- device scratch of the entry point that allocates nothing -----------------------------------------------

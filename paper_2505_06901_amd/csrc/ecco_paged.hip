@@ -58,6 +58,8 @@ __device__ __forceinline__ void store_out(args_t* a, size_t at, float v) {
     if (a->half) ((__attribute__((address_space(1))) _Float16*)a->out)[at] = (_Float16)v;
     else ((__attribute__((address_space(1))) float*)a->out)[at] = v;
 }
+// A row that sees nothing has no weights and gives zeros; one whose scores are no numbers has a denominator that is none, and gives NaN.
+__device__ __forceinline__ float normalised(float num, float den) { return den == 0.0f ? 0.0f : num / den; }
 // (a pointer that is read back is known to be global memory only by a cast there and back)
 __device__ __forceinline__ const uint32_t* global_words(const uint32_t* p) { return (const uint32_t*)in_global(p); }
 
@@ -516,7 +518,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(kWa
                 if (n_splits == 1) {
                     const float den = denominator(g);
                     const int token = r / grp;
-                    store_out(a, ((size_t)(seq.row0 + token) * a->Hq + hkv * grp + r - token * grp) * kGroup + dim, den > 0.0f ? sum / den : 0.0f);
+                    store_out(a, ((size_t)(seq.row0 + token) * a->Hq + hkv * grp + r - token * grp) * kGroup + dim, normalised(sum, den));
                 } else {
                     ws[(part + (size_t)r * n_splits) * kGroup + dim] = sum;
                 }
@@ -535,8 +537,8 @@ __global__ __launch_bounds__(kGroup) void attend_rows_merge_kernel(PagedArgs arg
     if (r >= seq.n_new * grp || seq.n_new * grp > args.few || ranges.y == 1) return;
     if (ranges.x < 0 || ranges.y < 1 || ((int64_t)ranges.x + ranges.y) * args.Hkv > n_wgs) return;  // not in the workspace
     const size_t at = ((size_t)ranges.x * args.Hkv + (size_t)hkv * ranges.y) * kernel_rows + (size_t)r * ranges.y, total = (size_t)n_wgs * kernel_rows;
-    const float v = merge_splits(args.ws + total * kGroup + at * 2, args.ws + at * kGroup + threadIdx.x, ranges.y);
-    store_out(a, ((size_t)(seq.row0 + token) * a->Hq + hkv * grp + r - token * grp) * kGroup + threadIdx.x, v);
+    const Merged v = merge_splits(args.ws + total * kGroup + at * 2, args.ws + at * kGroup + threadIdx.x, ranges.y);
+    store_out(a, ((size_t)(seq.row0 + token) * a->Hq + hkv * grp + r - token * grp) * kGroup + threadIdx.x, normalised(v.num, v.den));
 }
 
 // ---- many rows per key/value head ----------------------------------------------------------------------------------------
