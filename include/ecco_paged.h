@@ -35,7 +35,9 @@ extern "C" {
  * taken, no entry written, its slots -1, its kv_len 0 -- if not all of its rows lie below n_tokens, if it needs more than max_pages, or
  * if the pages that it and the sequences before it need are more than there are (one that needs none is served all the same).
  * Otherwise kv_len = seq_len + new_len.  q_start is the running sum of new_len, at most n_tokens; rows from q_start[B] on get slot -1.
- * Apart from free_left, which may be free_count, outputs must not overlap inputs: lengths are advanced by a copy of kv_len behind the step.
+ * Apart from free_left, which may be free_count, outputs must not overlap inputs.  Behind the step, lengths are advanced to the larger of seq_len and
+ * kv_len, element by element: a sequence that was not served then keeps its length, with it its pages and what their tokens hold, and may be
+ * offered the same tokens again.  (kv_len alone would make it 0 tokens long, and its pages nobody's.)
  * Errors: EINVAL (null), ESHAPE (B, max_pages, n_pages <= 0, n_tokens < 0, page_tokens, sizes over 2^31 - 1), EALIGN (4 bytes), EINVAL (kv_len is
  * seq_len or new_len), EHIP.  With n_tokens == 0 slots may be null. */
 int ecco_kv_pages_take(const int32_t* seq_len, const int32_t* new_len, int B, int page_tokens, int max_pages, int32_t* page_table,
@@ -79,7 +81,7 @@ int ecco_kv_append_paged_minmax(const ecco_model* mk, const ecco_model* mv, cons
  * enter the second product as two FP16 numbers (22 bits), or as one (11 bits) where out is FP16 and the sequence has many rows.  They are scaled so that
  * the largest is at FP16's top: whatever its size, a weight is off by 2^-40 of the largest at the most (few rows) or 2^-36 (many), or by its last bit.  The
  * same call gives the same bits; other bounds may cut the sums elsewhere.
- * A query that is not finite makes its own outputs NaN, and no others.
+ * A query that is not finite makes its own outputs NaN (zeros, if all its scores are minus infinity), and no others.
  * A block with a scale that is not finite (never written by the encoder) makes all rows of its sequence unspecified.
  * Errors: EINVAL (also a workspace too small), ESHAPE, EALIGN, EHIP.  n_tokens == 0 is a no-op. */
 size_t ecco_kv_attend_paged_workspace(int device, int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv);

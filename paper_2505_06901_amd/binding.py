@@ -384,7 +384,8 @@ def _pool(k_blocks, k_meta, v_blocks, v_meta):
 def ecco_kv_pages_take(seq_len, new_len, page_table, free_pages, free_count, page_tokens: int, n_tokens: int, free_left=None, q_start=None,
                        kv_len=None, slots=None):
     """seq_len, new_len int32 [B]; page_table int32 [B, max_pages], updated in place; free_pages int32 [n_pages]; free_count int32 [1], updated
-    in place unless free_left is another tensor.  Returns (q_start [B + 1], kv_len [B], slots [n_tokens])."""
+    in place unless free_left is another tensor.  Returns (q_start [B + 1], kv_len [B], slots [n_tokens]).  kv_len is 0 for sequences that are
+    not served: behind the step, torch.maximum(seq_len, kv_len, out=seq_len) advances the others and leaves those as they are."""
     B, max_pages = page_table.shape
     if q_start is None or kv_len is None or slots is None:
         import torch

@@ -84,3 +84,69 @@ def test_queries_that_are_not_finite_reach_their_own_outputs_only(dev, oracle, m
     assert torch.isnan(got[bad]).all()
     # the others may be scaled at other moments: the same but for the last bits
     assert torch.allclose(got[~bad].float(), clean[~bad].float(), rtol=0, atol=float(clean.float().abs().max()) * (2.0 ** -10 if half else 2.0 ** -18))
+
+
+def test_captured_steps_that_run_out_of_pages(dev, oracle, models):
+    """A whole step in a graph whose sequences grow until pages run out: those that are not served give zeros, keep their length, pages and tokens, and go on once
+    others have ended; at the end every page is back."""
+    B, Hq, Hkv, page, n_pages, max_pages, n_new = 4, 8, 2, 16, 9, 6, 5
+    rng = np.random.default_rng(8)
+    table, free, count, lens = ints(np.full((B, max_pages), -1), dev), ints(rng.permutation(n_pages), dev), ints([n_pages], dev), ints(np.zeros(B), dev)
+    pool = [torch.zeros((n_pages, Hkv, page, 64), dtype=torch.uint8, device=dev), torch.zeros((n_pages, Hkv, page), dtype=torch.int32, device=dev)] * 2
+    pool = [t.clone() for t in pool]
+    rows, new = B * n_new, ints(np.full(B, n_new), dev)
+    q, k, v = (torch.zeros((rows, h, 128), dtype=torch.float16, device=dev) for h in (Hq, Hkv, Hkv))
+    out, kv_len = torch.empty((rows, Hq, 128), dtype=torch.float32, device=dev), ints(np.zeros(B), dev)
+
+    def step():
+        q_start, _, slots = E.ecco_kv_pages_take(lens, new, table, free, count, page, rows, kv_len=kv_len)
+        E.ecco_kv_append_paged(*models, k, v, *pool, slots)
+        E.ecco_kv_attend_paged(*models, q, *pool, table, q_start, kv_len, n_new, max_pages * page, out=out)
+        torch.maximum(lens, kv_len, out=lens)
+
+    new.zero_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()  # (no new tokens: nothing changes)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    keys, values = [np.zeros((0, Hkv, 128), np.float16)] * B, [np.zeros((0, Hkv, 128), np.float16)] * B
+    decoded = lambda m, x: oracle.decode(m.centroids, m.code_lens, *oracle.encode(m.centroids, m.code_lens, x.reshape(-1, 128).view(np.uint16))).view(np.float16).reshape(x.shape)  # noqa: E731
+    refused = 0
+    for i in range(16):
+        count_new = rng.integers(0, n_new + 1, B) if i % 3 else np.full(B, n_new)
+        n = int(count_new.sum())
+        qh, (kh, vh) = queries(rows, Hq, 40 + i), (np.ascontiguousarray(x[0].transpose(1, 0, 2)) for x in W.kv_cache(1, Hkv, rows, 128, seed=60 + i))
+        for t, x in ((q, qh), (k, kh), (v, vh)):
+            t.copy_(torch.from_numpy(x))
+        new.copy_(ints(count_new, dev))
+        graph.replay()
+        torch.cuda.synchronize()
+        got, kv, row = out.cpu().numpy(), kv_len.cpu().numpy(), 0
+        for b, m in enumerate(count_new):
+            at = np.s_[row:row + m]
+            row += m
+            if kv[b] == 0 and len(keys[b]) + m > 0:  # not served
+                refused += 1
+                assert not got[at].any()
+                continue
+            if m:
+                keys[b], values[b] = np.concatenate([keys[b], decoded(models[0], kh[at])]), np.concatenate([values[b], decoded(models[1], vh[at])])
+            assert kv[b] == len(keys[b])
+            seen = np.repeat(np.arange(kv[b])[None, :] <= (kv[b] - m + np.arange(m))[:, None], Hq // Hkv, 0)
+            for h in range(Hkv):
+                o, e = R.attend(qh[at, h * 4:h * 4 + 4].reshape(-1, 128), keys[b][:, h], values[b][:, h], seen)
+                R.check_attend(got[at, h * 4:h * 4 + 4].reshape(-1, 128), o, {"element": e, "most": 0.0}, False, (i, b, h))
+        assert row == n and lens.tolist() == [len(x) for x in keys], i
+        if i % 5 == 4:  # the longest one has ended
+            b = int(np.argmax([len(x) for x in keys]))
+            keep = [0 if j == b else len(x) for j, x in enumerate(keys)]
+            E.ecco_kv_pages_release(lens, ints(keep, dev), table, free, count, page)
+            lens.copy_(ints(keep, dev))
+            keys[b], values[b] = keys[b][:0], values[b][:0]
+    assert refused > 0  # (the path was reached)
+    E.ecco_kv_pages_release(lens, ints(np.zeros(B), dev), table, free, count, page)
+    assert int(count) == n_pages and sorted(free.tolist()) == list(range(n_pages))
