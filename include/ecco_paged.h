@@ -83,6 +83,11 @@ int ecco_kv_append_paged_minmax(const ecco_model* mk, const ecco_model* mv, cons
  * same call gives the same bits; other bounds may cut the sums elsewhere.
  * A query that is not finite makes its own outputs NaN (zeros, if all its scores are minus infinity), and no others.
  * A block with a scale that is not finite (never written by the encoder) makes all rows of its sequence unspecified.
+ * The workspace never shrinks when n_tokens, B, max_new, max_kv or total_kv grows: one for a program's largest step serves all of them.  What it
+ * holds where max_new * Hq / Hkv is above 32 are mainly operands, 512 bytes per token and key/value head -- of min(total_kv, s * max_kv) tokens, s being the sequences
+ * that may have more rows than a token: min(B, n_tokens / 2), also where most of them bring a token each -- and up to 34 MB of parts (256 compute units).
+ * With fewer rows it is parts alone: at most 520 bytes for each of 32 rows, and of twice the compute units and one per sequence and head, if there are
+ * fewer of these than compute units; 0 for sequences of up to 256 tokens.
  * Errors: EINVAL (also a workspace too small), ESHAPE, EALIGN, EHIP.  n_tokens == 0 is a no-op. */
 size_t ecco_kv_attend_paged_workspace(int device, int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv);
 int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint16_t* q, int64_t q_stride,

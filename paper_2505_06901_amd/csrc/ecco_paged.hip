@@ -552,8 +552,6 @@ __global__ __launch_bounds__(kGroup) void attend_rows_merge_kernel(PagedArgs arg
 //       l takes dimension 32 d + l % 32 and the tokens 16 s + 4 (l / 32) + (0 1 2 3 8 9 10 11): those whose scores the lane holds after the
 //       first product, so that probabilities become B operands where they are
 // so a unit is copied to LDS as it is, and read from there without bank conflicts.
-constexpr int kUnitHalves = kUnitBlocks * kGroup;      // FP16 values of a unit's K, or V
-constexpr int kUnitBytes = 2 * kUnitHalves * 2;
 
 // Where sequences lie in the workspace and in the launch: running sums over the sequences
 struct Layout {
@@ -994,48 +992,6 @@ __global__ __launch_bounds__(kMergeThreads) void attend_tiles_merge_kernel(TileA
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------------
-struct Plan {
-    int few, few_rows, cut, units;               // sequences with up to `few` rows are decoded on the way: the kernel's rows, whether in ranges, units of the longest
-    int wide_tiles, tile_rows, wide_splits, wide_units;  // the others: tiles that there may be, their rows, ranges of the tokens, units in the workspace
-    size_t few_bytes, bytes;                     // of the workspace
-};
-constexpr size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
-Plan plan_of(int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv, int cus) {
-    Plan p{};
-    max_new = std::min(max_new, n_tokens);
-    const int grp = Hq / Hkv;
-    const long long rows = (long long)max_new * grp;
-    const bool wide = rows > kFewRows, all = wide && (long long)max_new * B == n_tokens;  // every sequence has as many rows
-    // Beside chunks, what is taken on the way is sequences with a token each, in the kernel that suits those.
-    const long long few = wide ? grp : rows;
-    p.few_rows = few <= 8 ? 8 : few <= 16 ? 16 : kFewRows;
-    p.few = all ? 0 : (int)few;
-    if (!all) {
-        // Into ranges where there are fewer sequences and heads than compute units, and sequences that one round of the wavefronts does not take
-        p.units = units_of(max_kv);
-        p.cut = B * (long long)Hkv < cus && B <= kRangeSequences && p.units > kRangeLeast;
-        if (p.cut) p.few_bytes = round_up((size_t)B * 8) + round_up((size_t)(B * Hkv + 2 * cus) * p.few_rows * (kGroup + 2) * sizeof(float));
-    }
-    p.bytes = p.few_bytes;
-    if (wide) {
-        // A tile of 256 rows reads what it needs once for twice the rows, but there have to be enough of them: a 2048-token prompt, 32/8 heads, 69.3 us
-        // with 512 tiles of 128 rows, 78.1 us with 256 of 256; four chunks of up to 1024 tokens over 8192, 684 us with 980, 625 us with 490.
-        p.tile_rows = (long long)n_tokens * grp / 256 * Hkv * 2 >= 3ll * cus ? 256 : 128;
-        const long long many = std::min<long long>(B, (long long)n_tokens * grp / ((long long)p.few + 1));  // sequences with more rows than `few`
-        const long long each = (rows + p.tile_rows - 1) / p.tile_rows;
-        p.wide_tiles = (int)(all ? each * B : std::min(each * many, (long long)n_tokens * grp / p.tile_rows + many));
-        const long long units = std::min<long long>((std::min<long long>(total_kv, (long long)many * max_kv)) / kUnitBlocks + many, 0x7FFFFFFF);
-        p.wide_units = (int)units;
-        // Split over the tokens where that makes a workgroup for every compute unit, and a range is worth its share of the merge: a chunk of 512 tokens
-        // over 4096, 128 tiles, 87.4 us whole, 71.7 us in two, 75.3 us in four; 64 tokens over 4096, 16 tiles, 99.1 us, in four 52.2 us, in eight
-        // 46.2 us; 1000 tokens over themselves, 128 tiles, 38.2 us, in two 40.1 us.
-        const long long wgs = (long long)p.wide_tiles * Hkv;
-        p.wide_splits = (int)std::min<long long>(std::min<long long>(std::max<long long>(1, cus / wgs), ((long long)max_kv + 511) / 512), 64);
-        p.bytes += 2 * round_up(((size_t)B + 1) * 4) + round_up((size_t)units * 4) + (size_t)units * Hkv * kUnitBytes;
-        if (p.wide_splits > 1) p.bytes += round_up((size_t)wgs * p.tile_rows * p.wide_splits * (kGroup + 2) * sizeof(float));
-    }
-    return p;
-}
 bool sizes_fit(int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv) {
     return n_tokens >= 0 && B > 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Hq / Hkv <= kGqaMaxGroup && max_new > 0 && max_kv > 0 && total_kv > 0 &&
            (long long)B * Hkv <= 0x7FFFFFFF && (long long)n_tokens * Hq <= 0x7FFFFFFF;
@@ -1047,7 +1003,7 @@ extern "C" {
 
 size_t ecco_kv_attend_paged_workspace(int device, int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv) {
     if (n_tokens == 0 || !sizes_fit(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv)) return 0;
-    return plan_of(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv, cu_count(device)).bytes;
+    return paged_workspace(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv, cu_count(device));
 }
 
 int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint16_t* q, int64_t q_stride,
@@ -1067,8 +1023,9 @@ int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint1
     if (model_ready(mk) != ECCO_OK || model_ready(mv) != ECCO_OK || mk->device != mv->device) return ECCO_EINVAL;
     if (n_tokens == 0) return ECCO_OK;
     const int dev_id = mk->device, cus = cu_count(dev_id), shift = __builtin_ctz((unsigned)page_tokens);
-    const Plan plan = plan_of(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv, cus);
-    if (plan.bytes > 0 && (!workspace || workspace_bytes < plan.bytes)) return ECCO_EINVAL;
+    const PagedPlan plan = paged_plan(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv, cus);
+    const size_t bytes = paged_workspace(n_tokens, B, Hq, Hkv, max_new, max_kv, total_kv, cus);
+    if (bytes > 0 && (!workspace || workspace_bytes < bytes)) return ECCO_EINVAL;
     const bool lk = mk->max_len > kPeekBits, lv = mv->max_len > kPeekBits;
     max_kv = std::min(max_kv, max_pages << shift);
     hipStream_t st = static_cast<hipStream_t>(stream);

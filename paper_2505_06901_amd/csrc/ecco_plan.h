@@ -1,4 +1,4 @@
-// How the attention kernels of the two-chain format are launched: wavefronts, tables and spans by sizes alone.  Host code without a
+// How the attention kernels of the two-chain format are launched: wavefronts, tables, spans and workspaces by sizes alone.  Host code without a
 // runtime call, so that every size can be looked at without a GPU; the constants are shared with the kernels (ecco_kernels.hip).
 #pragma once
 
@@ -157,6 +157,82 @@ inline GqaPlan rows_plan(int Sk, bool lk, int Sv, bool lv, int rows, size_t wgs,
     if (lk || lv) return rows_plan_of(rows > kGqaMaxGroup ? 8 : 12, kLdsWords, wk, wv, rows, units);
     if (rows_can_share(Sk, lk, Sv, lv, rows) && (cut || share_units(wgs, units, cus))) return rows_plan_of(8, kLdsWords / 2, wk, wv, rows, units);
     return rows_plan_of(units <= 8 && rows <= kGqaMaxGroup ? 8 : 12, kLdsWords, wk, wv, rows, units);
+}
+
+// ---- attention over pages: what is decoded on the way and what into the workspace, and how much of that there may be
+constexpr int kUnitBytes = 2 * kUnitBlocks * kGroup * 2;  // a unit's K and V as operands in the workspace
+struct PagedPlan {
+    int few, few_rows, cut, units;               // sequences with up to `few` rows are decoded on the way: the kernel's rows, whether in ranges, units of the longest
+    int wide_tiles, tile_rows, wide_splits, wide_units;  // the others: tiles that there may be, their rows, ranges of the tokens, units in the workspace
+    size_t few_bytes, bytes;                     // of the workspace
+};
+constexpr size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
+constexpr size_t kBytesMost = (size_t)1 << 60;  // where products of sizes stop: more than any memory
+constexpr size_t bytes_of(size_t a, size_t b) { return b != 0 && a > kBytesMost / b ? kBytesMost : a * b; }
+constexpr size_t kPartBytes = (kGroup + 2) * sizeof(float);  // of a row and a range: outputs, maximum, denominator
+constexpr int rows_bucket(int rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : kFewRows; }
+// of the ranges: (first, count) per sequence, and the parts of all that there may be
+inline size_t range_bytes(int B, int Hkv, int cus, int rows) { return round_up((size_t)B * 8) + round_up(((size_t)B * Hkv + 2 * (size_t)cus) * rows * kPartBytes); }
+// of the operands and the running sums beside them
+inline size_t operand_bytes(int B, int Hkv, int units) { return 2 * round_up(((size_t)B + 1) * 4) + round_up((size_t)units * 4) + bytes_of((size_t)units * kUnitBytes, Hkv); }
+// units of `many` sequences of up to max_kv tokens, and total_kv together
+inline int units_of_all(long long many, int max_kv, long long total_kv) { return (int)std::min<long long>(std::min(total_kv, many * max_kv) / kUnitBlocks + many, 0x7FFFFFFF); }
+constexpr int splits_most(int max_kv) { return (int)std::min<long long>(((long long)max_kv + 511) / 512, 64); }
+
+inline PagedPlan paged_plan(int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, long long total_kv, int cus) {
+    PagedPlan p{};
+    max_new = std::min(max_new, n_tokens);
+    const int grp = Hq / Hkv;
+    const long long rows = (long long)max_new * grp;
+    const bool wide = rows > kFewRows, all = wide && (long long)max_new * B == n_tokens;  // every sequence has as many rows
+    // Beside chunks, what is taken on the way is sequences with a token each, in the kernel that suits those.
+    const long long few = wide ? grp : rows;
+    p.few_rows = rows_bucket((int)few);
+    p.few = all ? 0 : (int)few;
+    if (!all) {
+        // Into ranges where there are fewer sequences and heads than compute units, and sequences that one round of the wavefronts does not take
+        p.units = units_of(max_kv);
+        p.cut = B * (long long)Hkv < cus && B <= kRangeSequences && p.units > kRangeLeast;
+        if (p.cut) p.few_bytes = range_bytes(B, Hkv, cus, p.few_rows);
+    }
+    p.bytes = p.few_bytes;
+    if (wide) {
+        // rows that the sequences have at the most, and sequences that have more than `few` of them: two tokens each, then
+        const long long tokens = std::min<long long>(n_tokens, (long long)max_new * B), many = all ? B : std::min<long long>(B, tokens / 2);
+        // A tile of 256 rows reads what it needs once for twice the rows, but there have to be enough of them: a 2048-token prompt, 32/8 heads, 69.3 us
+        // with 512 tiles of 128 rows, 78.1 us with 256 of 256; four chunks of up to 1024 tokens over 8192, 684 us with 980, 625 us with 490.
+        p.tile_rows = tokens * grp / 256 * Hkv * 2 >= 3ll * cus ? 256 : 128;
+        const long long each = (rows + p.tile_rows - 1) / p.tile_rows;
+        p.wide_tiles = (int)(all ? each * B : std::min(each * many, tokens * grp / p.tile_rows + many));
+        p.wide_units = units_of_all(many, max_kv, total_kv);
+        // Split over the tokens where that makes a workgroup for every compute unit, and a range is worth its share of the merge: a chunk of 512 tokens
+        // over 4096, 128 tiles, 87.4 us whole, 71.7 us in two, 75.3 us in four; 64 tokens over 4096, 16 tiles, 99.1 us, in four 52.2 us, in eight
+        // 46.2 us; 1000 tokens over themselves, 128 tiles, 38.2 us, in two 40.1 us.
+        const long long wgs = (long long)p.wide_tiles * Hkv;
+        p.wide_splits = (int)std::min<long long>(std::max<long long>(1, cus / wgs), splits_most(max_kv));
+        p.bytes += operand_bytes(B, Hkv, p.wide_units);
+        if (p.wide_splits > 1) p.bytes += round_up((size_t)wgs * p.tile_rows * p.wide_splits * kPartBytes);
+    }
+    return p;
+}
+// Bytes that the workspace is asked to have: what any step within these sizes takes, so that one that is allocated for a program's largest step
+// serves all of them.  (A plan by itself can take more for less: fewer sequences and heads than compute units are cut into ranges, fewer tiles
+// are split.)  Each part is the most of its own: of the ranges with as many sequences as are ever cut and the widest kernel, of the
+// operands with all sequences that may have many rows, of the splits with as many tiles of 128 rows as there are compute units.  (256-row tiles are at
+// least three for two compute units, so that they are not split.)
+inline size_t paged_workspace(int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, long long total_kv, int cus) {
+    max_new = std::min(max_new, n_tokens);
+    const int grp = Hq / Hkv, cut = std::min({B, kRangeSequences, (cus - 1) / Hkv});
+    const long long rows = (long long)max_new * grp;
+    size_t bytes = 0;
+    if (cut > 0 && units_of(max_kv) > kRangeLeast) bytes += range_bytes(cut, Hkv, cus, rows_bucket((int)std::min<long long>(rows, kFewRows / grp * grp)));
+    if (rows > kFewRows) {
+        const long long tokens = std::min<long long>(n_tokens, (long long)max_new * B), many = std::min<long long>(B, tokens / 2);
+        const long long tiles = std::min((rows + 127) / 128 * many, tokens * grp / 128 + many);
+        bytes += operand_bytes(B, Hkv, units_of_all(many, max_kv, total_kv));
+        if (splits_most(max_kv) > 1) bytes += round_up((size_t)std::min<long long>(cus, tiles * Hkv * splits_most(max_kv)) * 128 * kPartBytes);
+    }
+    return bytes;
 }
 
 }  // namespace ecco

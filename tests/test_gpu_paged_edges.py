@@ -150,3 +150,22 @@ def test_captured_steps_that_run_out_of_pages(dev, oracle, models):
     assert refused > 0  # (the path was reached)
     E.ecco_kv_pages_release(lens, ints(np.zeros(B), dev), table, free, count, page)
     assert int(count) == n_pages and sorted(free.tolist()) == list(range(n_pages))
+
+
+@pytest.mark.parametrize("half", [False, True])
+def test_one_workspace_for_every_step(dev, oracle, models, half):
+    """A workspace allocated for the largest step, and nothing behind it written, serves steps that are planned in other ways: ranges, none, splits, tiles of 256."""
+    Hq, Hkv, lens = 128, 8, [2100, 900, 40] + [70] * 29
+    c = Cache(dev, oracle, models, lens, Hkv, 16, 20)
+    steps = [[1] * 32, [1] * 31, [1, 1, 1], [2, 2, 1], [64, 1, 1], [800, 300, 40], [2, 900], [1] + [0] * 31, [1200, 1, 0, 3]]
+    largest = E.ecco_kv_attend_paged_workspace(1300, 32, Hq, Hkv, 1200, 2100, sum(lens))
+    memory = torch.full((largest + 4096,), 0xA5, dtype=torch.uint8, device=dev)
+    for i, new in enumerate(steps):
+        kv = lens[:len(new)]
+        q = torch.from_numpy(queries(sum(new), Hq, 30 + i)).to(dev)
+        args = (*models, q, *c.pool, c.table[:len(new)].contiguous(), ints(np.concatenate([[0], np.cumsum(new)]), dev), ints(kv, dev), max(new), max(kv), sum(kv))
+        out = [torch.empty(q.shape, dtype=torch.float16 if half else torch.float32, device=dev) for _ in range(2)]
+        E.ecco_kv_attend_paged(*args, workspace=memory[:largest], out=out[0])
+        E.ecco_kv_attend_paged(*args, out=out[1])
+        assert torch.equal(*out) and torch.isfinite(out[0]).all(), new
+        assert bool((memory[largest:] == 0xA5).all()), new
