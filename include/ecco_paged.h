@@ -88,7 +88,8 @@ int ecco_kv_append_paged_minmax(const ecco_model* mk, const ecco_model* mv, cons
  * that may have more rows than a token: min(B, n_tokens / 2), also where most of them bring a token each -- and up to 34 MB of parts (256 compute units).
  * With fewer rows it is parts alone: at most 520 bytes for each of 32 rows, and of twice the compute units and one per sequence and head, if there are
  * fewer of these than compute units; 0 for sequences of up to 256 tokens.
- * Errors: EINVAL (also a workspace too small), ESHAPE, EALIGN, EHIP.  n_tokens == 0 is a no-op. */
+ * Errors: EINVAL (also a workspace too small), ESHAPE, EALIGN, EHIP.  n_tokens == 0 is a no-op, also with 0 sequences and bounds of 0; with rows
+ * all of these are at least 1. */
 size_t ecco_kv_attend_paged_workspace(int device, int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv);
 int ecco_kv_attend_paged(const ecco_model* mk, const ecco_model* mv, const uint16_t* q, int64_t q_stride,
                          const void* k_blocks, const uint32_t* k_meta, const void* v_blocks, const uint32_t* v_meta,

@@ -992,8 +992,10 @@ __global__ __launch_bounds__(kMergeThreads) void attend_tiles_merge_kernel(TileA
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------------
+// (a step without rows may have nothing else either)
 bool sizes_fit(int n_tokens, int B, int Hq, int Hkv, int max_new, int max_kv, int64_t total_kv) {
-    return n_tokens >= 0 && B > 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Hq / Hkv <= kGqaMaxGroup && max_new > 0 && max_kv > 0 && total_kv > 0 &&
+    const int least = n_tokens == 0 ? 0 : 1;
+    return n_tokens >= 0 && B >= least && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Hq / Hkv <= kGqaMaxGroup && max_new >= least && max_kv >= least && total_kv >= least &&
            (long long)B * Hkv <= 0x7FFFFFFF && (long long)n_tokens * Hq <= 0x7FFFFFFF;
 }
 
