@@ -169,3 +169,66 @@ def test_one_workspace_for_every_step(dev, oracle, models, half):
         E.ecco_kv_attend_paged(*args, out=out[1])
         assert torch.equal(*out) and torch.isfinite(out[0]).all(), new
         assert bool((memory[largest:] == 0xA5).all()), new
+
+
+def test_a_step_without_rows(dev, models):
+    pool = [torch.zeros((3, 2, 16, 64), dtype=torch.uint8, device=dev), torch.zeros((3, 2, 16), dtype=torch.int32, device=dev)] * 2
+    q = torch.zeros((0, 8, 128), dtype=torch.float16, device=dev)
+    for B in (0, 2):
+        out = E.ecco_kv_attend_paged(*models, q, *pool, ints(np.zeros((B, 4)), dev), ints(np.zeros(B + 1), dev), ints(np.zeros(B), dev), 0, 0)
+        assert out.shape == q.shape
+
+
+@pytest.mark.parametrize("B,new,kv,bounds,fits", [
+    # (max_new, max_kv, total_kv) that the lengths exceed; how many sequences come before the first that does not fit
+    (6, 40, 300, (40, 300, 700), 2),          # 21 + 6 units of 32 tokens for ten each
+    (6, 40, 300, (40, 300, 1), 0),            # six for ten
+    (130, 9, 200, (9, 200, 1), 18),           # 130 units for seven each; the layout in a launch of its own
+    (130, 9, 200, (9, 200, 12800), 75),       # 400 + 130: the first that does not fit is in the second set of 64
+    (2, (40, 260), 90, (40, 90, 180), 1),     # four tiles for two and nine
+    (66, (9,) * 65 + (130,), 40, (9, 40, 66 * 40), 65),  # as many tiles as sequences
+])
+@pytest.mark.parametrize("half", [False, True])
+def test_many_rows_beyond_the_bounds(dev, oracle, models, B, new, kv, bounds, fits, half):
+    """Lengths on the device that need more of the workspace or the launch than the bounds provide: sequences ahead of the first that does not fit are what they
+    are, it and those behind it are left unwritten, and so is what lies behind the workspace."""
+    Hq, Hkv, new = 8, 2, [new] * B if isinstance(new, int) else list(new)
+    c = Cache(dev, oracle, models, [kv] * B, Hkv, 16, 50)
+    n, guard = sum(new), 1 << 20
+    q = queries(n, Hq, 51)
+    size = E.ecco_kv_attend_paged_workspace(n, B, Hq, Hkv, *bounds)
+    memory = torch.full((size + guard,), 0xA5, dtype=torch.uint8, device=dev)
+    out = torch.full((n + 4, Hq, 128), float("nan"), dtype=torch.float16 if half else torch.float32, device=dev)
+    E.ecco_kv_attend_paged(*models, torch.from_numpy(q).to(dev), *c.pool, c.table, ints(np.concatenate([[0], np.cumsum(new)]), dev), ints([kv] * B, dev), *bounds, memory[:size], out[:n])
+    got, row = out.cpu().numpy(), 0
+    assert bool((memory[size:] == 0xA5).all())
+    for b in range(fits):
+        if b % 8 == 0 or b >= fits - 2:
+            want, bound = c.want(q[row:row + new[b]], b, new[b], kv)
+            R.check_attend(got[row:row + new[b]], want, {"element": bound, "most": float(np.abs(c.values[b].astype(np.float64)).max())}, half, b)
+        row += new[b]
+    assert np.isfinite(got[:row]).all() and np.isnan(got[row:]).all()
+
+
+@pytest.mark.parametrize("starts,lens,whole", [
+    ([0, 1, 3, 4], [300, 2 ** 31 - 1, 100], {0: (0, 1), 2: (3, 4)}),    # a length behind max_kv: its sequence sees what lies there
+    ([0, 1, 3, 2 ** 31 - 1], [300, 500, -4], {0: (0, 1), 1: (1, 3)}),   # rows behind n_tokens: none
+    ([0, 1, -7, 1], [300, 500, 100], {0: (0, 1)}),                      # starts that do not ascend: none
+    ([0, 1, 3, 4], [300, 500, -4], {0: (0, 1), 1: (1, 3), 2: (3, 4)}),  # a negative length: sees nothing
+])
+def test_few_rows_beyond_the_bounds(dev, oracle, models, starts, lens, whole):
+    """Every row that the bounds cover is what it is, and rows of no sequence are left as they were."""
+    kv = [300, 500, 100]
+    c = Cache(dev, oracle, models, kv, 2, 16, 60)
+    q = queries(4, 8, 61)
+    out = torch.full((6, 8, 128), float("nan"), dtype=torch.float32, device=dev)
+    E.ecco_kv_attend_paged(*models, torch.from_numpy(q).to(dev), *c.pool, c.table, ints(starts, dev), ints(lens, dev), 2, 512, 900, out=out[:4])
+    got, rows = out.cpu().numpy(), set(range(6))
+    for b, (i, j) in whole.items():
+        t = max(min(lens[b], kv[b]), 0)
+        want, bound = c.want(q[i:j], b, j - i, t)
+        R.check_attend(got[i:j], want, {"element": bound, "most": 0.0}, False, b)
+        rows -= set(range(i, j))
+    if lens[1] > 512:
+        rows -= {1, 2}
+    assert np.isnan(got[sorted(rows)]).all()
