@@ -47,7 +47,10 @@ int ecco_kv_pages_take(const int32_t* seq_len, const int32_t* new_len, int B, in
 /* Puts the pages back that sequences no longer need: of a sequence that goes from seq_len to keep_len tokens (0: it is done) the
  * entries ceil(keep_len / page_tokens) .. ceil(seq_len / page_tokens) - 1, sequence by sequence, onto the stack.  keep_len is taken as
  * 0..seq_len.  Entries that are no pages of the pool, or behind max_pages, are left out, and so is what would exceed n_pages.
- * page_table is not changed.  Arguments and errors as above; free_pages is written from free_pages[count] on. */
+ * page_table is not changed.  Arguments and errors as above; free_pages is written from free_pages[count] on.
+ * Nothing counts who holds a page: one that is released twice -- by two sequences that share it, or by one in two calls -- is on the stack
+ * twice and will be given to two sequences.  A program that lets sequences share pages counts their holders itself, and leaves a shared
+ * page out with a keep_len behind it until the last one ends. */
 int ecco_kv_pages_release(const int32_t* seq_len, const int32_t* keep_len, int B, int page_tokens, int max_pages, const int32_t* page_table,
                           int32_t* free_pages, const int32_t* free_count, int32_t* free_left, int n_pages, void* stream);
 

@@ -401,7 +401,7 @@ def ecco_kv_pages_take(seq_len, new_len, page_table, free_pages, free_count, pag
 
 def ecco_kv_pages_release(seq_len, keep_len, page_table, free_pages, free_count, page_tokens: int, free_left=None):
     """Pages of the tokens keep_len .. seq_len go back onto free_pages; free_count is updated in place unless free_left is another tensor.
-    Returns the tensor with the new count."""
+    Returns the tensor with the new count.  A page that two sequences share goes back once for each: it must be released for the last one only."""
     B, max_pages = page_table.shape
     free_left = free_count if free_left is None else free_left
     n_pages = free_pages.numel()

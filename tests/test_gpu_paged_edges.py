@@ -232,3 +232,12 @@ def test_few_rows_beyond_the_bounds(dev, oracle, models, starts, lens, whole):
     if lens[1] > 512:
         rows -= {1, 2}
     assert np.isnan(got[sorted(rows)]).all()
+
+
+def test_shared_pages_are_given_back_once(dev):
+    """Two sequences share their first three pages: the first to end keeps them (keep_len behind them), the last one gives all back."""
+    table, free, count = ints([[4, 1, 7, 0, -1], [4, 1, 7, 3, 6]], dev), ints([2, 5, -1, -1, -1, -1, -1, -1], dev), ints([2], dev)
+    E.ecco_kv_pages_release(ints([60, 70], dev), ints([60, 48], dev), table, free, count, 16)
+    assert int(count) == 4 and free.tolist()[:4] == [2, 5, 3, 6]
+    E.ecco_kv_pages_release(ints([60, 48], dev), ints([0, 48], dev), table, free, count, 16)
+    assert int(count) == 8 and free.tolist() == [2, 5, 3, 6, 4, 1, 7, 0]
