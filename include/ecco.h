@@ -214,7 +214,7 @@ int ecco_device_info(int device, int* compute_units, int* memory_clock_khz, int*
  *               caller, contents irrelevant before and after) receives the partial results and a second small kernel
  *               merges them;  with n_splits == 1 workspace may be null.
  * Every K and V block is decoded once for all query heads of its group; products run on the matrix cores with the
- * probabilities rounded to FP16 (the denominator sums the rounded values).  Slots of the cache at or behind seq_len
+ * probabilities, 1 for the largest, as two FP16 numbers each (those below 2^-25 are 0; the denominator sums them in FP32).  Slots of the cache at or behind seq_len
  * may be uninitialised.  Calls that share a workspace must not overlap.
  * Errors: EINVAL, ESHAPE (sizes, Hq % Hkv, group > 16, n_splits), EALIGN, EHIP. */
 size_t ecco_kv_attend_gqa_workspace(int B, int Hq, int n_splits);

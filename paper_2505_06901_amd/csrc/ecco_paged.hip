@@ -737,8 +737,8 @@ __global__ __launch_bounds__(kExpandWaves * 64) void attend_expand_kernel(TileAr
 // FP32 one goes through a product of its own (the error against 64 bits 1.1e-6 in a step of two 450-token chunks over 4096); for FP16 outputs it is left out: half a step of a
 // weight, at random, adds 19 % to the error that the outputs' own rounding makes (2.5e-4 for 2.1e-4), and without it the chunk above takes 441 us
 // instead of 572.
-// What bounds it: a 4096-token chunk over 8192, 32/8 heads, FP16 outputs, 397 to 403 us for 412 GFLOP; in a run of 422 us the matrix cores were busy 54 % of
-// the time at 1.87 GHz.  Power holds the clock there: with zeros for queries and values the whole call took 347 us beside 439, and the library's
+// What bounds it: a 4096-token chunk over 8192, 32/8 heads, FP16 outputs, 408 to 411 us for 412 GFLOP; in a run of 434 us the matrix cores were busy 53 % of
+// the time at 1.85 GHz.  Power holds the clock there: with zeros for queries and values the whole call took 347 us beside 439, and the library's
 // product of 8192^3 reaches 1.16 PFLOP/s with random values and 1.72 with zeros.  Two wavefronts of a SIMD held in opposite phases by barriers:
 // 501 us beside 422; exponentials left out, for the measurement alone: the call 401 us beside 433.
 constexpr float kScoreToExp2 = 0.08838834764831845f * 1.4426950408889634f;  // log2(e) / sqrt(128)
