@@ -89,6 +89,8 @@ int ecco_kv_append_paged_minmax(const ecco_model* mk, const ecco_model* mv, cons
  * The workspace never shrinks when n_tokens, B, max_new, max_kv or total_kv grows: one for a program's largest step serves all of them.  What it
  * holds where max_new * Hq / Hkv is above 32 are mainly operands, 512 bytes per token and key/value head -- of min(total_kv, s * max_kv) tokens, s being the sequences
  * that may have more rows than a token: min(B, n_tokens / 2), also where most of them bring a token each -- and up to 34 MB of parts (256 compute units).
+ * Where that is too much, a step's chunks and its single tokens can be two calls, each with the table's, q_start's and kv_len's entries of its own sequences and
+ * their bounds, over the same q and out.
  * With fewer rows it is parts alone: at most 520 bytes for each of 32 rows, and of twice the compute units and one per sequence and head, if there are
  * fewer of these than compute units; 0 for sequences of up to 256 tokens.
  * Errors: EINVAL (also a workspace too small), ESHAPE, EALIGN, EHIP.  n_tokens == 0 is a no-op, also with 0 sequences and bounds of 0; with rows

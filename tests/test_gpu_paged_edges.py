@@ -241,3 +241,26 @@ def test_shared_pages_are_given_back_once(dev):
     assert int(count) == 4 and free.tolist()[:4] == [2, 5, 3, 6]
     E.ecco_kv_pages_release(ints([60, 48], dev), ints([0, 48], dev), table, free, count, 16)
     assert int(count) == 8 and free.tolist() == [2, 5, 3, 6, 4, 1, 7, 0]
+
+
+@pytest.mark.parametrize("half", [False, True])
+def test_chunks_and_tokens_called_apart(dev, oracle, models, half):
+    """A step's chunk and its single tokens in two calls over the same rows, each with its own sequences and bounds: neither touches the other's rows, and each asks for the
+    workspace of its own."""
+    new, kv, Hq, Hkv = [64] + [1] * 7, [900, 40, 2000, 1, 333, 700, 64, 65], 32, 8
+    c = Cache(dev, oracle, models, kv, Hkv, 16, 70)
+    q = queries(sum(new), Hq, 71)
+    starts, lens, out = ints(np.concatenate([[0], np.cumsum(new)]), dev), ints(kv, dev), torch.full(q.shape, float("nan"), dtype=torch.float16 if half else torch.float32, device=dev)
+    qd = torch.from_numpy(q).to(dev)
+    for i, j in ((0, 1), (1, 8)):
+        size = E.ecco_kv_attend_paged_workspace(sum(new), j - i, Hq, Hkv, max(new[i:j]), max(kv[i:j]), sum(kv[i:j]))
+        assert size < 20 * 2 ** 20
+        E.ecco_kv_attend_paged(*models, qd, *c.pool, c.table[i:j], starts[i:j + 1], lens[i:j], max(new[i:j]), max(kv[i:j]), sum(kv[i:j]),
+                               torch.empty((size,), dtype=torch.uint8, device=dev), out)
+        done = int(starts[j])
+        assert torch.isfinite(out[:done]).all() and torch.isnan(out[done:]).all()
+    got = out.cpu().numpy()
+    for b, (n, t) in enumerate(zip(new, kv)):
+        at = np.s_[int(starts[b]):int(starts[b + 1])]
+        want, bound = c.want(q[at], b, n, t)
+        R.check_attend(got[at], want, {"element": bound, "most": float(np.abs(c.values[b].astype(np.float64)).max())}, half, b)
